@@ -45,7 +45,10 @@ typedef enum {
 
 typedef enum {
     FREQKV_BF16 = 0,            /* cache holds bfloat16; fp16 MFMA operands, fp32 accumulate */
-    FREQKV_F32  = 1             /* cache holds float32; fp32 FMA throughout                  */
+    FREQKV_F32  = 1,            /* cache holds float32; fp32 FMA throughout                  */
+    /* codes of one byte with a scale for each block of tokens of a head, see freqkv_scales_t; for the entry points that say so */
+    FREQKV_INT8 = 2,            /* two's complement, -127 .. 127                             */
+    FREQKV_E4M3 = 3             /* 1 sign, 4 exponent and 3 mantissa bits, no infinity, largest value 448 */
 } freqkv_dtype_t;
 
 /* layout.flags */
@@ -354,6 +357,99 @@ FREQKV_API freqkv_status_t freqkv_attend_prefill(const void* q, const void* k, c
                                       float* lse, const freqkv_layout_t* layout, int n_q_heads,
                                       int n_kv_heads, int head_dim, int cur_len, int q_len,
                                       double rope_base, void* stream);
+
+/*
+ * A cache held in 8 bits: codes of one byte (layout.dtype FREQKV_INT8 or FREQKV_E4M3) and a scale for each block of block_tokens rows of a head;
+ * the value of a channel is code * scale.  The codes lie as `layout` says, strides in elements (bytes), which like the base pointers are multiples of 16; the
+ * scale of (layer, batch, head, block) is at [layer * stride_layer + batch * stride_batch + head * stride_head + block], strides in floats.
+ * Keys are held without the rotary embedding, as in the other caches.
+ */
+typedef struct freqkv_scales {
+    float*  k;                  /* device; 4-byte aligned                                            */
+    float*  v;
+    int32_t block_tokens;       /* 16, 32, 64 or 128                                                 */
+    int32_t reserved;
+    int64_t stride_layer;       /* in floats                                                         */
+    int64_t stride_batch;
+    int64_t stride_head;        /* at least ceil(rows in use / block_tokens)                         */
+} freqkv_scales_t;
+
+/*
+ * Rows become codes: rows [row, row + n_rows) of a bf16 or fp32 cache (k, v, layout) the rows [code_row, code_row + n_rows) of an 8-bit one.
+ *   code_rows  optional DEVICE array [batch] of int32 in place of code_row: first row of each sequence; a sequence whose rows would not lie in
+ *              [0, layout8.token_capacity) is left alone
+ * A block whose first row is among them gets a new scale, the smallest by which no value of its new rows exceeds the largest code: a number of 8 significant
+ * bits for int8 (value / 127 rounded up), a power of two for e4m3; at least 2^-100, and 0 where all of them are zero.  A block that holds rows
+ * ahead of code_row already keeps its scale or, where a new row needs a larger one, has it doubled until that fits, and its older codes are rounded again: rows
+ * may come one by one, and each stays within one step of the block's scale (int8; e4m3 codes but lose bits below its least exponent) of what it was.
+ * Quotients are rounded to the nearest code, ties to the even one, exactly.  Where a value of the new rows of a block is infinite or NaN the block's scale becomes NaN,
+ * and its values with it.  Rows behind code_row + n_rows of the last block are not looked at or written.
+ * head_dim a multiple of 16, up to 256 (FREQKV_E_UNSUPPORTED otherwise); both layouts have the same n_layers and batch.  No workspace.  n_rows 0: FREQKV_NOOP.
+ */
+FREQKV_API freqkv_status_t freqkv_quantize(const void* k, const void* v, const freqkv_layout_t* layout, int row, void* k8, void* v8,
+                                const freqkv_layout_t* layout8, const freqkv_scales_t* scales, int code_row, const int32_t* code_rows /* device */,
+                                int n_rows, int n_heads, int head_dim, void* stream);
+
+/* Codes become rows: code * scale, rounded once to the type of the rows (for a freqkv_compress of what the 8-bit cache holds, for one).  As freqkv_quantize. */
+FREQKV_API freqkv_status_t freqkv_dequantize(const void* k8, const void* v8, const freqkv_layout_t* layout8, const freqkv_scales_t* scales, int code_row,
+                                  void* k, void* v, const freqkv_layout_t* layout, int row, int n_rows, int n_heads, int head_dim, void* stream);
+
+/* Buffer plan of freqkv_attend_q8.  HOST only.  Ranges as for freqkv_attend_plan; 1 <= q_len <= cur_len; q_dtype FREQKV_BF16 or FREQKV_F32. */
+FREQKV_API freqkv_status_t freqkv_attend_q8_plan(const freqkv_layout_t* layout8, int q_dtype, int n_q_heads, int n_kv_heads, int head_dim, int cur_len,
+                                      int q_len, freqkv_attend_plan_t* out);
+
+/*
+ * Attention over an 8-bit cache: of one token per sequence (q_len 1, as freqkv_attend_decode) or of the q_len tokens of a chunk, whose keys and values are
+ * the last q_len cached rows (as freqkv_attend_prefill).  Query i of a sequence of n rows sits at row n - q_len + i and attends to the rows up to there.
+ * Rotary embedding, head grouping and scaling as there.
+ *   q, out    [n_layers][batch][n_q_heads][q_len][head_dim], dense, of type q_dtype (FREQKV_BF16 or FREQKV_F32)
+ *   lse       optional [n_layers][batch][n_q_heads][q_len] fp32
+ *   k8, v8    codes as freqkv_quantize writes them (no NaN codes), through layout8; scales: theirs
+ *   cur_lens  optional DEVICE array [batch] of int32: cached rows of each sequence, clamped to [0, cur_len]; cur_len is then their upper bound.  Queries
+ *             that sit ahead of row 0 (n < q_len) see nothing: their results are zero, their lse -inf.  Rows at and beyond a sequence's length are not read.
+ *   layout8.workspace  freqkv_attend_q8_plan(...).workspace_bytes, 256-byte aligned; with less the rows are cut into fewer chunks, down to one
+ * head_dim 64, 128 or 256.  Operands of the matrix cores are fp16, exact for the codes, 11 bits for turned keys, queries and softmax weights; with
+ * q_dtype FREQKV_F32 each is a sum of two, 22 bits.  Sums are fp32.  Queries and scales may have any finite magnitude.  q, out and lse must be 16-byte aligned.
+ */
+FREQKV_API freqkv_status_t freqkv_attend_q8(const void* q, const void* k8, const void* v8, void* out, float* lse, const freqkv_layout_t* layout8,
+                                 const freqkv_scales_t* scales, int q_dtype, int n_q_heads, int n_kv_heads, int head_dim, int cur_len, int q_len,
+                                 const int32_t* cur_lens /* device */, double rope_base, void* stream);
+
+/* Buffer plan of freqkv_attend_weights.  HOST only.  Ranges as for freqkv_attend_plan; 1 <= q_len <= cur_len. */
+FREQKV_API freqkv_status_t freqkv_attend_weights_plan(const freqkv_layout_t* layout, int n_q_heads, int n_kv_heads, int head_dim, int cur_len, int q_len,
+                                           freqkv_attend_plan_t* out);
+
+/*
+ * The attention that every cached row got: weights[row] = sum over the queries that see the row, and over the heads that share its KV head, of
+ * exp(score - lse of the query), added to what is there with accumulate 1, in its place with 0.  The queries are those of the last q_len rows, as in
+ * freqkv_attend_decode (q_len 1) and freqkv_attend_prefill, which give their lse.
+ *   q         [n_layers][batch][n_q_heads][q_len][head_dim], dense, layout.dtype, un-rotated
+ *   k         the keys, through `layout` (bf16 or fp32); values are not read
+ *   lse       [n_layers][batch][n_q_heads][q_len] fp32; a query whose lse is -inf adds nothing
+ *   weights   [n_layers][batch][n_kv_heads][layout.token_capacity] fp32; rows at and beyond a sequence's length are left as they were
+ *   cur_lens  optional DEVICE array [batch], as in freqkv_attend_q8; queries that sit ahead of row 0 add nothing
+ *   layout.workspace  freqkv_attend_weights_plan(...).workspace_bytes, 256-byte aligned
+ * head_dim 64, 128 or 256.  Scores are good to 22 bits whatever the type; the order of the sums, and so their bits, depend on the sizes alone.
+ */
+FREQKV_API freqkv_status_t freqkv_attend_weights(const void* q, const void* k, const float* lse, float* weights, const freqkv_layout_t* layout,
+                                      int n_q_heads, int n_kv_heads, int head_dim, int cur_len, int q_len, const int32_t* cur_lens /* device */,
+                                      int accumulate, double rope_base, void* stream);
+
+/*
+ * Eviction by such weights, in the place of a compression: of the rows [n_sink, n - n_recent) of every head of a sequence of n rows the `keep` with the largest
+ * weights stay, each KV head its own, in their order (of equal weights the lower rows; NaN counts as less than all others); sinks stay, the latest n_recent
+ * rows follow: [sinks | kept | recent].  K and V move in place.  Where at most `keep` rows compete nothing moves.
+ *   weights      [n_layers][batch][n_heads][layout.token_capacity] fp32
+ *   weights_out  optional, same shape, may be `weights`: weights of the rows as they lie after the call; rows from the new length to cur_len become 0, so that the
+ *                tokens that come next start from there
+ *   kept         [n_layers][batch][n_heads][keep] int32: rows that stayed, ascending; where nothing moved the rows that competed, and -1 behind them
+ *   cur_lens     optional DEVICE array [batch] of int32, clamped to [0, cur_len], cur_len then being their upper bound
+ *   new_lens     optional DEVICE array [batch] of int32: rows of each sequence after the call; not cur_lens itself
+ * head_dim a multiple of 8; keep >= 1.  After the call rows at and beyond a sequence's new length hold unspecified values.  No workspace.
+ */
+FREQKV_API freqkv_status_t freqkv_evict(void* k, void* v, const float* weights, float* weights_out, int32_t* kept, const freqkv_layout_t* layout, int n_heads,
+                             int head_dim, int cur_len, int n_sink, int n_recent, int keep, const int32_t* cur_lens /* device */,
+                             int32_t* new_lens /* device */, void* stream);
 
 /*
  * Diagnostic of the factored transform (variant 6), used by the tests to check its stages one by one: runs

@@ -13,7 +13,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_PKG, "lib", "libfreqkv.so")
 _lib = None
 
-BF16, F32 = 0, 1
+BF16, F32, INT8, E4M3 = 0, 1, 2, 3
 FLAG_NO_RESCALE = 0x1
 FLAG_DROPPING = 0x2
 FLAG_RETAIN_HIGH = 0x4
@@ -80,6 +80,14 @@ class AttendPlan(C.Structure):
     ]
 
 
+class Scales(C.Structure):
+    """struct freqkv_scales (include/freqkv.h)."""
+    _fields_ = [
+        ("k", C.c_void_p), ("v", C.c_void_p), ("block_tokens", C.c_int32), ("reserved", C.c_int32),
+        ("stride_layer", C.c_int64), ("stride_batch", C.c_int64), ("stride_head", C.c_int64),
+    ]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -122,6 +130,16 @@ def load() -> C.CDLL:
     lib.freqkv_attend_prefill.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, LP,
                                           C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, C.c_double, C.c_void_p]
     lib.freqkv_attend_prefill.restype = C.c_int
+    SP, vp, ci = C.POINTER(Scales), C.c_void_p, C.c_int
+    lib.freqkv_quantize.argtypes = [vp, vp, LP, ci, vp, vp, LP, SP, ci, vp, ci, ci, ci, vp]
+    lib.freqkv_dequantize.argtypes = [vp, vp, LP, SP, ci, vp, vp, LP, ci, ci, ci, ci, vp]
+    lib.freqkv_attend_q8_plan.argtypes = [LP, ci, ci, ci, ci, ci, ci, C.POINTER(AttendPlan)]
+    lib.freqkv_attend_q8.argtypes = [vp, vp, vp, vp, vp, LP, SP, ci, ci, ci, ci, ci, ci, vp, C.c_double, vp]
+    lib.freqkv_attend_weights_plan.argtypes = [LP, ci, ci, ci, ci, ci, C.POINTER(AttendPlan)]
+    lib.freqkv_attend_weights.argtypes = [vp, vp, vp, vp, LP, ci, ci, ci, ci, ci, vp, ci, C.c_double, vp]
+    lib.freqkv_evict.argtypes = [vp, vp, vp, vp, vp, LP, ci, ci, ci, ci, ci, ci, vp, vp, vp]
+    for name in ("quantize", "dequantize", "attend_q8_plan", "attend_q8", "attend_weights_plan", "attend_weights", "evict"):
+        getattr(lib, "freqkv_" + name).restype = C.c_int
     lib.freqkv_prepare.argtypes = [C.c_int, C.c_uint32, C.c_int, C.c_int, C.c_double, C.c_void_p]
     lib.freqkv_prepare.restype = C.c_int
     lib.freqkv_debug_compress_kernel.argtypes = [LP, C.c_int, C.c_int, C.c_int, C.c_int, C.c_double]
@@ -311,6 +329,73 @@ def attend_prefill(q, k, v, out, lse, layout: Layout, n_q_heads: int, n_kv_heads
     return _check(rc) if check else rc
 
 
+def quantize(k, v, layout: Layout, row: int, k8, v8, layout8: Layout, scales: Scales, code_row: int, n_rows: int, n_heads: int,
+             head_dim: int, code_rows=None, stream=None, check: bool = True) -> int:
+    """freqkv_quantize.  k8, v8: int8 or float8_e4m3fn device tensors, through layout8; code_rows: int32 device tensor [batch] in
+    place of code_row, or None."""
+    rc = load().freqkv_quantize(_dev_ptr(k), _dev_ptr(v), C.byref(layout), row, _dev_ptr(k8), _dev_ptr(v8), C.byref(layout8),
+                                C.byref(scales), code_row, _dev_ptr(code_rows), n_rows, n_heads, head_dim, _stream_ptr(stream))
+    return _check(rc) if check else rc
+
+
+def dequantize(k8, v8, layout8: Layout, scales: Scales, code_row: int, k, v, layout: Layout, row: int, n_rows: int, n_heads: int,
+               head_dim: int, stream=None, check: bool = True) -> int:
+    """freqkv_dequantize: rows [code_row, code_row + n_rows) of the codes become rows [row, ..) of k, v."""
+    rc = load().freqkv_dequantize(_dev_ptr(k8), _dev_ptr(v8), C.byref(layout8), C.byref(scales), code_row, _dev_ptr(k), _dev_ptr(v),
+                                  C.byref(layout), row, n_rows, n_heads, head_dim, _stream_ptr(stream))
+    return _check(rc) if check else rc
+
+
+def attend_q8_plan(layout8: Layout, q_dtype: int, n_q_heads: int, n_kv_heads: int, head_dim: int, cur_len: int, q_len: int = 1,
+                   check: bool = True):
+    """freqkv_attend_q8_plan: returns (status, AttendPlan).  Host arithmetic only."""
+    out = AttendPlan()
+    rc = load().freqkv_attend_q8_plan(C.byref(layout8), q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, C.byref(out))
+    if check:
+        _check(rc)
+    return rc, out
+
+
+def attend_q8(q, k8, v8, out, lse, layout8: Layout, scales: Scales, q_dtype: int, n_q_heads: int, n_kv_heads: int, head_dim: int,
+              cur_len: int, q_len: int = 1, cur_lens=None, rope_base: float = 10000.0, stream=None, check: bool = True) -> int:
+    """freqkv_attend_q8.  q, out: dense [layer, batch, q_head, q_len, dim] device tensors of q_dtype (BF16 or F32); cur_lens: int32
+    device tensor [batch] or None."""
+    rc = load().freqkv_attend_q8(_dev_ptr(q), _dev_ptr(k8), _dev_ptr(v8), _dev_ptr(out), _dev_ptr(lse), C.byref(layout8),
+                                 C.byref(scales), q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, _dev_ptr(cur_lens),
+                                 float(rope_base), _stream_ptr(stream))
+    return _check(rc) if check else rc
+
+
+def attend_weights_plan(layout: Layout, n_q_heads: int, n_kv_heads: int, head_dim: int, cur_len: int, q_len: int = 1,
+                        check: bool = True):
+    """freqkv_attend_weights_plan: returns (status, AttendPlan).  Host arithmetic only."""
+    out = AttendPlan()
+    rc = load().freqkv_attend_weights_plan(C.byref(layout), n_q_heads, n_kv_heads, head_dim, cur_len, q_len, C.byref(out))
+    if check:
+        _check(rc)
+    return rc, out
+
+
+def attend_weights(q, k, lse, weights, layout: Layout, n_q_heads: int, n_kv_heads: int, head_dim: int, cur_len: int, q_len: int = 1,
+                   cur_lens=None, accumulate: bool = False, rope_base: float = 10000.0, stream=None, check: bool = True) -> int:
+    """freqkv_attend_weights.  lse: fp32 [layer, batch, q_head, q_len] as attend_decode and attend_prefill return it; weights: fp32
+    device tensor [layer, batch, kv_head, layout.token_capacity]."""
+    rc = load().freqkv_attend_weights(_dev_ptr(q), _dev_ptr(k), _dev_ptr(lse), _dev_ptr(weights), C.byref(layout), n_q_heads,
+                                      n_kv_heads, head_dim, cur_len, q_len, _dev_ptr(cur_lens), 1 if accumulate else 0,
+                                      float(rope_base), _stream_ptr(stream))
+    return _check(rc) if check else rc
+
+
+def evict(k, v, weights, weights_out, kept, layout: Layout, n_heads: int, head_dim: int, cur_len: int, n_sink: int, n_recent: int,
+          keep: int, cur_lens=None, new_lens=None, stream=None, check: bool = True) -> int:
+    """freqkv_evict.  weights: fp32 [layer, batch, kv_head, layout.token_capacity]; weights_out: the same shape (or weights itself) or
+    None; kept: int32 [layer, batch, kv_head, keep]; cur_lens, new_lens: int32 device tensors [batch] or None."""
+    rc = load().freqkv_evict(_dev_ptr(k), _dev_ptr(v), _dev_ptr(weights), _dev_ptr(weights_out), _dev_ptr(kept), C.byref(layout),
+                             n_heads, head_dim, cur_len, n_sink, n_recent, keep, _dev_ptr(cur_lens), _dev_ptr(new_lens),
+                             _stream_ptr(stream))
+    return _check(rc) if check else rc
+
+
 def profile_enable(on: bool) -> None:
     _check(load().freqkv_profile_enable(1 if on else 0))
 
@@ -364,7 +449,7 @@ def layout_for(k, *, batch_dim: bool = True, workspace=None, tap=None, flags: in
         raise ValueError("expected a [layer, batch, head, token, dim] tensor")
     if k.stride(4) != 1:
         raise ValueError("channel stride must be 1")
-    dt = {torch.bfloat16: BF16, torch.float32: F32}[k.dtype]
+    dt = {torch.bfloat16: BF16, torch.float32: F32, torch.int8: INT8, torch.float8_e4m3fn: E4M3}[k.dtype]
     L = Layout()
     L.dtype = dt
     L.n_layers, L.batch = k.shape[0], k.shape[1]
@@ -378,3 +463,16 @@ def layout_for(k, *, batch_dim: bool = True, workspace=None, tap=None, flags: in
     if tap is not None:
         L.tap_f32 = tap.data_ptr()
     return L
+
+
+def scales_for(k_scale, v_scale, block_tokens: int) -> Scales:
+    """Scales of an 8-bit cache from two fp32 torch tensors [layer, batch, head, block] of the same strides, the last one 1."""
+    import torch
+    if k_scale.dim() != 4 or k_scale.dtype != torch.float32 or v_scale.dtype != torch.float32 or k_scale.shape != v_scale.shape:
+        raise ValueError("expected two fp32 [layer, batch, head, block] tensors")
+    if k_scale.stride() != v_scale.stride() or (k_scale.shape[3] > 1 and k_scale.stride(3) != 1):
+        raise ValueError("scales of K and V have the same strides, that of a block 1")
+    S = Scales()
+    S.k, S.v, S.block_tokens = k_scale.data_ptr(), v_scale.data_ptr(), block_tokens
+    S.stride_layer, S.stride_batch, S.stride_head = k_scale.stride(0), k_scale.stride(1), k_scale.stride(2)
+    return S

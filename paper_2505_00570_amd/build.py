@@ -14,7 +14,7 @@ LIB_DIR = os.path.join(PKG, "lib")
 OBJ_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(LIB_DIR, "libfreqkv.so")
 SOURCES = ["freqkv_kernels.hip", "freqkv_fast.hip", "freqkv_nearfar.hip", "freqkv_nearfar_units.hip",
-           "freqkv_attend.hip", "freqkv_prefill.hip", "freqkv_api.hip"]
+           "freqkv_attend.hip", "freqkv_prefill.hip", "freqkv_q8.hip", "freqkv_evict.hip", "freqkv_api.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 # -packed-fp32-ops off: the device compiler must not form v_pk_{add,mul,fma}_f32 from float code.  The
@@ -65,7 +65,7 @@ def build(verbose: bool = True) -> str:
         return obj
 
     # the files are independent: compile them side by side (hipcc itself is single-threaded per file)
-    with ThreadPoolExecutor(max_workers=min(4, len(SOURCES))) as pool:
+    with ThreadPoolExecutor(max_workers=min(6, len(SOURCES))) as pool:
         objs = list(pool.map(compile_one, SOURCES))
     tmp = LIB + ".tmp%d" % os.getpid()
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs

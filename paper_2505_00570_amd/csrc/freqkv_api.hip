@@ -479,7 +479,8 @@ freqkv_status_t check_attend(const freqkv_layout_t* L, int n_q, int n_kv, int d,
 struct RopeKey {
     int device, d;
     double base;
-    bool operator<(const RopeKey& o) const { return std::tie(device, d, base) < std::tie(o.device, o.d, o.base); }
+    bool turns = false;                 // a TurnTable; else RopeEntry
+    bool operator<(const RopeKey& o) const { return std::tie(device, d, base, turns) < std::tie(o.device, o.d, o.base, o.turns); }
 };
 std::map<RopeKey, BasisEntry> g_rope;
 // What chunk-wise calls keep per device at most: of these tables (those of decode calls count, which are kept whatever their number), and of the cos/sin below.
@@ -487,11 +488,12 @@ constexpr int kMostTables = 16;
 
 // ws: where a call has its table if there is none yet and none is to be allocated, as its stream is being captured or there are kMostTables, or if there is no
 // memory for it; null: a caller that allocates.
-freqkv_status_t get_rope_table(int d, double base, hipStream_t st, RopeEntry** out, void* ws = nullptr)
+freqkv_status_t get_rope_table(int d, double base, hipStream_t st, RopeEntry** out, void* ws = nullptr, bool turns = false)
 {
     int dev = 0;
     HIP_TRY(hipGetDevice(&dev));
-    RopeKey key{dev, d, base};
+    RopeKey key{dev, d, base, turns};
+    auto fill = [&](void* to) { return turns ? launch_turn_table(to, d, base, st) : launch_rope_table((RopeEntry*)to, d, base, st); };
     std::lock_guard<std::mutex> lock(g_mu);
     auto it = g_rope.find(key);
     if (it == g_rope.end()) {
@@ -504,19 +506,19 @@ freqkv_status_t get_rope_table(int d, double base, hipStream_t st, RopeEntry** o
             keep = cap == hipStreamCaptureStatusNone && held < kMostTables;
         }
         BasisEntry e;
-        e.bytes = (size_t)d * sizeof(RopeEntry);
+        e.bytes = turns ? turn_table_bytes(d) : (size_t)d * sizeof(RopeEntry);
         hipError_t err = keep ? hipMalloc(&e.ptr, e.bytes) : hipErrorOutOfMemory;
         if (err != hipSuccess) {
             if (keep) (void)hipGetLastError();
             if (ws) {
-                HIP_TRY(launch_rope_table((RopeEntry*)ws, d, base, st));
+                HIP_TRY(fill(ws));
                 *out = (RopeEntry*)ws;
                 return FREQKV_OK;
             }
             set_error("hipMalloc(rotary table)", err);
             return FREQKV_E_ALLOC;
         }
-        err = launch_rope_table((RopeEntry*)e.ptr, d, base, st);
+        err = fill(e.ptr);
         if (err == hipSuccess) err = hipEventCreateWithFlags(&e.ready, hipEventDisableTiming);
         if (err == hipSuccess) err = hipEventRecord(e.ready, st);
         if (err != hipSuccess) {
@@ -685,7 +687,7 @@ const char* freqkv_status_string(freqkv_status_t s)
 
 const char* freqkv_last_error(void) { return g_last_error; }
 
-int freqkv_version(void) { return 200; }
+int freqkv_version(void) { return 300; }
 
 freqkv_status_t freqkv_plan(const freqkv_layout_t* layout, int n_heads, int head_dim, int cur_len,
                             int window, int n_sink, double retain_ratio, freqkv_plan_t* out)
@@ -1673,6 +1675,403 @@ freqkv_status_t freqkv_attend_prefill(const void* q, const void* k, const void* 
         HIP_TRY(launch_attend_prefill(g, direct ? &tab : nullptr, (const _Float16*)(ws + p.off_kr), (const _Float16*)(ws + p.off_vt), qp, cs, op,
                                       lse ? lse + head0 * q_len : nullptr, part_acc, part_ml, st));
         HIP_TRY(prof_end(st, &sp));
+    }
+    return FREQKV_OK;
+}
+
+// ---------------------------------------------------------------- 8-bit caches, attention weights, eviction
+namespace {
+// Room for a rotary table ahead of the rest of a workspace, for calls that may not keep one (get_rope_table).
+constexpr size_t kTableBytes = turn_table_bytes(256);
+static_assert(kTableBytes % 256 == 0, "what follows is aligned");
+
+bool good_layout(const freqkv_layout_t* L, int multiple, int head_dim)
+{
+    if (!L || L->n_layers < 1 || L->batch < 1 || L->token_capacity < 1) return false;
+    if (L->pointer_table != 0 && L->pointer_table != 1) return false;
+    if (L->flags & ~(FREQKV_FLAG_NO_RESCALE | FREQKV_FLAG_DROPPING | FREQKV_FLAG_RETAIN_HIGH | FREQKV_FLAG_SINGLE_FOLD | FREQKV_FLAG_TWO_LEVEL_FOLD | FREQKV_FLAG_DENSE)) return false;
+    if (L->stride_token < head_dim || L->stride_token % multiple || L->stride_head % multiple || L->stride_batch % multiple) return false;
+    if (!L->pointer_table && L->stride_layer % multiple) return false;
+    return L->stride_head >= 0 && L->stride_batch >= 0;
+}
+
+bool eight_bit(const freqkv_layout_t* L) { return L->dtype == FREQKV_INT8 || L->dtype == FREQKV_E4M3; }
+int q8_format(const freqkv_layout_t& L) { return L.dtype == FREQKV_INT8 ? kInt8 : kE4M3; }
+
+bool good_scales(const freqkv_scales_t* s, int* shift)
+{
+    if (!s || !s->k || !s->v || ((uintptr_t)s->k | (uintptr_t)s->v) & 3) return false;
+    if (s->stride_batch < 0 || s->stride_head < 0) return false;
+    for (*shift = 4; *shift <= 7; ++*shift)
+        if (s->block_tokens == 1 << *shift) return true;
+    return false;
+}
+
+// Base pointers of K and V, layer by layer; false where one is missing or not on a 16-byte boundary.
+bool layer_bases(const void* k, const void* v, const freqkv_layout_t& L, int elem, std::vector<char*>* out)
+{
+    if (!k || !v) return false;
+    out->resize((size_t)2 * L.n_layers);
+    for (int l = 0; l < L.n_layers; ++l) {
+        for (int kv = 0; kv < 2; ++kv) {
+            const void* root = kv ? v : k;
+            char* p = L.pointer_table ? (char*)((void* const*)root)[l] : (char*)root + (long long)l * L.stride_layer * elem;
+            if (!p || ((uintptr_t)p & 15)) return false;
+            (*out)[(size_t)2 * l + kv] = p;
+        }
+    }
+    return true;
+}
+
+constexpr int kLayersPerPass = kMaxSlabs / 2;
+
+void slabs_of(const std::vector<char*>& bases, int l0, int layers, SlabTable* tab)
+{
+    memset(tab, 0, sizeof(*tab));
+    for (int i = 0; i < 2 * layers; ++i) tab->base[i] = bases[(size_t)2 * l0 + i];
+}
+
+// Both directions; code_rows: quantise only.
+freqkv_status_t q8_move(bool quantize, const void* k, const void* v, const freqkv_layout_t* layout, int row, const void* k8, const void* v8,
+                        const freqkv_layout_t* layout8, const freqkv_scales_t* scales, int code_row, const int32_t* code_rows, int n_rows, int n_heads,
+                        int head_dim, void* stream)
+{
+    g_last_error[0] = 0;
+    int shift = 0;
+    if (!layout || !layout8 || n_heads < 1 || head_dim < 16) return FREQKV_E_INVALID;
+    if (layout->dtype != FREQKV_BF16 && layout->dtype != FREQKV_F32) return FREQKV_E_INVALID;
+    if (!eight_bit(layout8) || !good_layout(layout, 8, head_dim) || !good_layout(layout8, 16, head_dim) || !good_scales(scales, &shift)) return FREQKV_E_INVALID;
+    if (head_dim % 16 || head_dim > 256) return FREQKV_E_UNSUPPORTED;
+    if (layout->n_layers != layout8->n_layers || layout->batch != layout8->batch) return FREQKV_E_INVALID;
+    if (n_rows < 0 || row < 0 || row > layout->token_capacity - n_rows) return FREQKV_E_INVALID;
+    if (code_rows ? n_rows > layout8->token_capacity || ((uintptr_t)code_rows & 3) : code_row < 0 || code_row > layout8->token_capacity - n_rows) return FREQKV_E_INVALID;
+    const int elem = layout->dtype == FREQKV_BF16 ? 2 : 4;
+    std::vector<char*> bases, bases8;
+    if (!layer_bases(k, v, *layout, elem, &bases) || !layer_bases(k8, v8, *layout8, 1, &bases8)) return FREQKV_E_INVALID;
+    if (n_rows == 0) return FREQKV_NOOP;
+
+    Q8MoveGeom g;
+    memset(&g, 0, sizeof(g));
+    g.format = q8_format(*layout8);
+    g.elem_bytes = elem;
+    g.d = head_dim;
+    g.block_shift = shift;
+    g.n_heads = n_heads;
+    const long long hts = (long long)layout->batch * n_heads, tokens = 1LL << shift;
+    // a device array may name any row: one block more than aligned rows have
+    const long long n_blk = !quantize ? ((long long)n_rows * (head_dim / 16) + kDequantPerWg - 1) / kDequantPerWg
+                            : code_rows ? (n_rows + 2 * tokens - 2) / tokens
+                                        : (code_row + (long long)n_rows - 1) / tokens - code_row / tokens + 1;
+    if (n_blk * hts >= 1LL << 23 || (long long)n_rows * (head_dim / 16) >= 1LL << 30) return FREQKV_E_UNSUPPORTED;
+    g.hts = (int)hts;
+    g.n_rows = n_rows;
+    g.row = row;
+    g.code_row = code_row;
+    g.code_rows = code_rows;
+    g.capacity = layout8->token_capacity;
+    g.n_blk = (int)n_blk;
+    g.by_blk = divisor(g.n_blk);
+    g.by_heads = divisor(n_heads);
+    g.by_pieces = divisor(quantize ? head_dim / 8 : head_dim / 16);
+    g.stride_batch = layout->stride_batch * elem;
+    g.stride_head = layout->stride_head * elem;
+    g.stride_token = layout->stride_token * elem;
+    g.code_batch = layout8->stride_batch;
+    g.code_head = layout8->stride_head;
+    g.code_token = layout8->stride_token;
+    g.scale_layer = scales->stride_layer;
+    g.scale_batch = scales->stride_batch;
+    g.scale_head = scales->stride_head;
+    for (int l0 = 0; l0 < layout->n_layers; l0 += kLayersPerPass) {
+        const int layers = std::min(layout->n_layers - l0, kLayersPerPass);
+        SlabTable rows, codes;
+        slabs_of(bases, l0, layers, &rows);
+        slabs_of(bases8, l0, layers, &codes);
+        g.k_scale = scales->k + l0 * scales->stride_layer;
+        g.v_scale = scales->v + l0 * scales->stride_layer;
+        if (quantize) HIP_TRY(launch_quantize(rows, codes, g, 2 * layers, (hipStream_t)stream));
+        else          HIP_TRY(launch_dequantize(codes, rows, g, 2 * layers, (hipStream_t)stream));
+    }
+    return FREQKV_OK;
+}
+
+struct Q8Shape {
+    long long units_all, units;         // all; of a pass
+    int M, parts, n_split, chunk;
+    size_t ml_offset, workspace_bytes;
+
+    void cut(long long ns, int cur_len, int d)
+    {
+        chunk = (int)round_up((cur_len + ns - 1) / ns, kQ8StepRows);
+        n_split = (cur_len + chunk - 1) / chunk;
+        const size_t states = n_split > 1 ? (size_t)units * M * n_split : 0;
+        ml_offset = kTableBytes + (size_t)round_up((long long)(states * d * sizeof(float)), 256);
+        workspace_bytes = ml_offset + states * 2 * sizeof(float);
+    }
+};
+
+freqkv_status_t check_q8(const freqkv_layout_t* L, int q_dtype, int n_q, int n_kv, int d, int cur_len, int q_len, Q8Shape* out)
+{
+    if (!L || !eight_bit(L) || (q_dtype != FREQKV_BF16 && q_dtype != FREQKV_F32)) return FREQKV_E_INVALID;
+    if (n_kv < 1 || n_q < 1 || n_q % n_kv || d < 8 || q_len < 1 || cur_len < 1) return FREQKV_E_INVALID;
+    if (d != 64 && d != 128 && d != 256) return FREQKV_E_UNSUPPORTED;
+    if (!good_layout(L, 16, d) || cur_len > L->token_capacity || q_len > cur_len) return FREQKV_E_INVALID;
+    // rows of a head are addressed by 32-bit byte offsets, some steps past the last one
+    if (((long long)cur_len + 1024) * L->stride_token >= (1LL << 32)) return FREQKV_E_UNSUPPORTED;
+    Q8Shape s;
+    s.units_all = (long long)L->n_layers * L->batch * n_kv;
+    s.units = (long long)std::min(L->n_layers, kLayersPerPass) * L->batch * n_kv;
+    const long long M = (long long)(n_q / n_kv) * q_len;
+    if (M >= 1 << 20 || s.units >= 1 << 20 || s.units_all * M >= 1LL << 31) return FREQKV_E_UNSUPPORTED;
+    s.M = (int)M;
+    s.parts = (s.M + kQ8Queries - 1) / kQ8Queries;
+    const long long most = (cur_len + kQ8StepRows - 1) / kQ8StepRows;
+    s.cut(std::min(most, std::max(1LL, 512 / (s.units * s.parts))), cur_len, d);
+    if (s.units * s.n_split >= 1 << 23) return FREQKV_E_UNSUPPORTED;
+    *out = s;
+    return FREQKV_OK;
+}
+
+struct WeightShape {
+    AttShape a;
+    long long units;                    // of a pass
+    int M, n_chunk, chunk, q_tiles, n_split, split_tiles, key_blocks;
+    size_t off_factors, off_parts, workspace_bytes;
+};
+
+freqkv_status_t check_weights(const freqkv_layout_t* L, int n_q, int n_kv, int d, int cur_len, int q_len, WeightShape* out)
+{
+    WeightShape w;
+    memset((void*)&w, 0, sizeof(w));
+    freqkv_status_t rc = check_attend(L, n_q, n_kv, d, cur_len, &w.a);
+    if (rc < 0) return rc;
+    if (q_len < 1 || q_len > cur_len) return FREQKV_E_INVALID;
+    w.units = (long long)std::min(L->n_layers, kLayersPerPass) * L->batch * n_kv;
+    const long long M = (long long)w.a.G * q_len;
+    if (M >= 1 << 20 || w.units >= 1 << 20) return FREQKV_E_UNSUPPORTED;
+    w.M = (int)M;
+    w.workspace_bytes = kTableBytes;
+    if (w.M <= kWeightFew) {
+        const long long most = (cur_len + kTurnStep - 1) / kTurnStep, ns = std::min(most, std::max(1LL, 1024 / w.units));
+        w.chunk = (int)round_up((cur_len + ns - 1) / ns, kTurnStep);
+        w.n_chunk = (cur_len + w.chunk - 1) / w.chunk;
+        if (w.units * w.n_chunk >= 1 << 23) return FREQKV_E_UNSUPPORTED;
+    } else {
+        w.q_tiles = (w.M + kWeightTile - 1) / kWeightTile;
+        w.key_blocks = (cur_len + kWeightKeys - 1) / kWeightKeys;
+        const long long wgs = w.units * w.key_blocks;
+        const long long ns = std::min((long long)w.q_tiles, std::max(1LL, 1024 / wgs));
+        w.split_tiles = (int)((w.q_tiles + ns - 1) / ns);
+        w.n_split = (w.q_tiles + w.split_tiles - 1) / w.split_tiles;
+        if (wgs * w.n_split >= 1 << 23 || w.units * w.q_tiles >= 1 << 23) return FREQKV_E_UNSUPPORTED;
+        w.off_factors = kTableBytes + (size_t)w.units * w.q_tiles * weight_operand_bytes(d);
+        w.off_parts = w.off_factors + (size_t)w.units * w.q_tiles * kWeightTile * sizeof(float2);
+        w.workspace_bytes = w.off_parts + (w.n_split > 1 ? (size_t)w.n_split * w.units * cur_len * sizeof(float) : 0);
+    }
+    *out = w;
+    return FREQKV_OK;
+}
+}  // namespace
+
+freqkv_status_t freqkv_quantize(const void* k, const void* v, const freqkv_layout_t* layout, int row, void* k8, void* v8, const freqkv_layout_t* layout8,
+                                const freqkv_scales_t* scales, int code_row, const int32_t* code_rows, int n_rows, int n_heads, int head_dim, void* stream)
+{
+    return q8_move(true, k, v, layout, row, k8, v8, layout8, scales, code_row, code_rows, n_rows, n_heads, head_dim, stream);
+}
+
+freqkv_status_t freqkv_dequantize(const void* k8, const void* v8, const freqkv_layout_t* layout8, const freqkv_scales_t* scales, int code_row, void* k, void* v,
+                                  const freqkv_layout_t* layout, int row, int n_rows, int n_heads, int head_dim, void* stream)
+{
+    return q8_move(false, k, v, layout, row, k8, v8, layout8, scales, code_row, nullptr, n_rows, n_heads, head_dim, stream);
+}
+
+freqkv_status_t freqkv_attend_q8_plan(const freqkv_layout_t* layout8, int q_dtype, int n_q_heads, int n_kv_heads, int head_dim, int cur_len, int q_len,
+                                      freqkv_attend_plan_t* out)
+{
+    if (!out) return FREQKV_E_INVALID;
+    Q8Shape s;
+    freqkv_status_t rc = check_q8(layout8, q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, &s);
+    if (rc < 0) return rc;
+    memset(out, 0, sizeof(*out));
+    out->n_split = s.n_split;
+    out->chunk_rows = s.chunk;
+    out->heads_together = std::min(s.M, kQ8Queries);
+    out->workspace_bytes = s.workspace_bytes;
+    const double seen = (double)q_len * (cur_len - q_len) + 0.5 * (double)q_len * (q_len + 1);
+    const double e = q_dtype == FREQKV_BF16 ? 2.0 : 4.0;
+    out->bytes_algorithmic = (double)s.units_all * (2.0 * cur_len * head_dim + 2.0 * s.M * head_dim * e);
+    out->flops = (double)s.units_all * (s.M / q_len) * 4.0 * head_dim * seen;
+    return FREQKV_OK;
+}
+
+freqkv_status_t freqkv_attend_q8(const void* q, const void* k8, const void* v8, void* out, float* lse, const freqkv_layout_t* layout8,
+                                 const freqkv_scales_t* scales, int q_dtype, int n_q_heads, int n_kv_heads, int head_dim, int cur_len, int q_len,
+                                 const int32_t* cur_lens, double rope_base, void* stream)
+{
+    g_last_error[0] = 0;
+    Q8Shape s;
+    int shift = 0;
+    freqkv_status_t rc = check_q8(layout8, q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, &s);
+    if (rc < 0) return rc;
+    if (!q || !out || !good_scales(scales, &shift)) return FREQKV_E_INVALID;
+    if (((uintptr_t)q | (uintptr_t)out | (uintptr_t)lse) & 15 || ((uintptr_t)cur_lens & 3)) return FREQKV_E_INVALID;
+    if (!(rope_base >= 0.0) || !(rope_base < 1e30)) return FREQKV_E_INVALID;
+    const freqkv_layout_t& L = *layout8;
+    std::vector<char*> bases;
+    if (!layer_bases(k8, v8, L, 1, &bases)) return FREQKV_E_INVALID;
+    // (a workspace planned at another length: fewer chunks)
+    while (s.n_split > 1 && s.workspace_bytes > L.workspace_bytes) s.cut(s.n_split - 1, cur_len, head_dim);
+    if (!L.workspace || ((uintptr_t)L.workspace & 255) || L.workspace_bytes < s.workspace_bytes) return FREQKV_E_WORKSPACE;
+    char* const ws = (char*)L.workspace;
+    hipStream_t st = (hipStream_t)stream;
+    RopeEntry* rt = nullptr;
+    rc = get_rope_table(head_dim, rope_base, st, &rt, ws, true);
+    if (rc < 0) return rc;
+    const int upl = L.batch * n_kv_heads, elem = q_dtype == FREQKV_BF16 ? 2 : 4;
+    for (int l0 = 0; l0 < L.n_layers; l0 += kLayersPerPass) {
+        const int layers = std::min(L.n_layers - l0, kLayersPerPass);
+        SlabTable tab;
+        slabs_of(bases, l0, layers, &tab);
+        Q8AttGeom g;
+        memset(&g, 0, sizeof(g));
+        g.format = q8_format(L);
+        g.f32 = elem == 4;
+        g.d = head_dim; g.M = s.M; g.q_len = q_len; g.parts = s.parts;
+        g.n_kv = n_kv_heads; g.units = layers * upl; g.units_per_layer = upl;
+        g.cur_len = cur_len; g.cur_lens = cur_lens;
+        g.block_shift = shift;
+        g.n_split = s.n_split; g.chunk = s.chunk;
+        g.by_split = divisor(s.n_split); g.by_layer = divisor(upl); g.by_kv = divisor(n_kv_heads); g.by_q = divisor(q_len);
+        g.code_batch = L.stride_batch; g.code_head = L.stride_head; g.code_token = L.stride_token;
+        g.scale_layer = scales->stride_layer; g.scale_batch = scales->stride_batch; g.scale_head = scales->stride_head;
+        g.k_scale = scales->k + l0 * scales->stride_layer;
+        g.v_scale = scales->v + l0 * scales->stride_layer;
+        g.qscale = (float)(1.4426950408889634 / std::sqrt((double)head_dim));
+        const long long head0 = (long long)l0 * upl * s.M;
+        const char* qp = (const char*)q + head0 * head_dim * elem;
+        char* op = (char*)out + head0 * head_dim * elem;
+        float* const ls = lse ? lse + head0 : nullptr;
+        float* const pa = (float*)(ws + kTableBytes);
+        float* const pm = (float*)(ws + s.ml_offset);
+        ProfSpan sp;
+        HIP_TRY(prof_begin(st, 3, &sp));
+        HIP_TRY(launch_attend_q8(tab, g, qp, turn_table(rt, head_dim), pa, pm, op, ls, st));
+        HIP_TRY(prof_end(st, &sp));
+        AttGeom m;
+        memset(&m, 0, sizeof(m));
+        m.d = head_dim; m.units = g.units; m.G = s.M; m.n_split = s.n_split;
+        HIP_TRY(launch_attend_merge(m, elem, pa, pm, op, ls, st));
+    }
+    return FREQKV_OK;
+}
+
+freqkv_status_t freqkv_attend_weights_plan(const freqkv_layout_t* layout, int n_q_heads, int n_kv_heads, int head_dim, int cur_len, int q_len,
+                                           freqkv_attend_plan_t* out)
+{
+    if (!out) return FREQKV_E_INVALID;
+    WeightShape w;
+    freqkv_status_t rc = check_weights(layout, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, &w);
+    if (rc < 0) return rc;
+    memset(out, 0, sizeof(*out));
+    out->n_split = w.M <= kWeightFew ? w.n_chunk : w.n_split;
+    out->chunk_rows = w.M <= kWeightFew ? w.chunk : kWeightKeys;
+    out->heads_together = std::min(w.M, w.M <= kWeightFew ? kWeightFew : kWeightTile);
+    out->workspace_bytes = w.workspace_bytes;
+    const double seen = (double)q_len * (cur_len - q_len) + 0.5 * (double)q_len * (q_len + 1);
+    out->bytes_algorithmic = (double)w.a.units_all * ((double)cur_len * (head_dim * w.a.elem + 4.0) + (double)w.M * (head_dim * w.a.elem + 4.0));
+    out->flops = (double)w.a.units_all * w.a.G * 2.0 * head_dim * seen;
+    return FREQKV_OK;
+}
+
+freqkv_status_t freqkv_attend_weights(const void* q, const void* k, const float* lse, float* weights, const freqkv_layout_t* layout, int n_q_heads,
+                                      int n_kv_heads, int head_dim, int cur_len, int q_len, const int32_t* cur_lens, int accumulate, double rope_base,
+                                      void* stream)
+{
+    g_last_error[0] = 0;
+    WeightShape w;
+    freqkv_status_t rc = check_weights(layout, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, &w);
+    if (rc < 0) return rc;
+    if (!q || !lse || !weights || ((uintptr_t)q & 15) || (((uintptr_t)lse | (uintptr_t)weights | (uintptr_t)cur_lens) & 3)) return FREQKV_E_INVALID;
+    if (accumulate != 0 && accumulate != 1) return FREQKV_E_INVALID;
+    if (!(rope_base >= 0.0) || !(rope_base < 1e30)) return FREQKV_E_INVALID;
+    const freqkv_layout_t& L = *layout;
+    std::vector<char*> bases;
+    if (!layer_bases(k, k, L, w.a.elem, &bases)) return FREQKV_E_INVALID;
+    if (!L.workspace || ((uintptr_t)L.workspace & 255) || L.workspace_bytes < w.workspace_bytes) return FREQKV_E_WORKSPACE;
+    char* const ws = (char*)L.workspace;
+    hipStream_t st = (hipStream_t)stream;
+    RopeEntry* rope = nullptr;
+    rc = get_rope_table(head_dim, rope_base, st, &rope, ws, true);
+    if (rc < 0) return rc;
+    const TurnTable rt = turn_table(rope, head_dim);
+    const int upl = w.a.batch * n_kv_heads;
+    for (int l0 = 0; l0 < w.a.n_layers; l0 += kLayersPerPass) {
+        const int layers = std::min(w.a.n_layers - l0, kLayersPerPass);
+        SlabTable tab;
+        memset(&tab, 0, sizeof(tab));
+        for (int i = 0; i < layers; ++i) tab.base[i] = bases[(size_t)2 * (l0 + i)];
+        WeightGeom g;
+        memset(&g, 0, sizeof(g));
+        g.elem_bytes = w.a.elem; g.d = head_dim; g.M = w.M; g.q_len = q_len;
+        g.n_kv = n_kv_heads; g.units = layers * upl; g.units_per_layer = upl;
+        g.cur_len = cur_len; g.cur_lens = cur_lens; g.accumulate = accumulate; g.capacity = L.token_capacity;
+        g.n_chunk = w.n_chunk; g.chunk = w.chunk; g.q_tiles = w.q_tiles; g.n_split = w.n_split; g.split_tiles = w.split_tiles; g.key_blocks = w.key_blocks;
+        g.by_chunk = divisor(w.n_chunk); g.by_layer = divisor(upl); g.by_kv = divisor(n_kv_heads); g.by_q = divisor(q_len);
+        g.by_keys = divisor(w.key_blocks); g.by_split = divisor(w.n_split);
+        g.stride_batch = L.stride_batch; g.stride_head = L.stride_head; g.stride_token = L.stride_token;
+        g.qscale = (float)(1.4426950408889634 / std::sqrt((double)head_dim));
+        const long long head0 = (long long)l0 * upl * w.M;
+        const char* qp = (const char*)q + head0 * head_dim * w.a.elem;
+        float* const to = weights + (long long)l0 * upl * L.token_capacity;
+        if (w.M <= kWeightFew) {
+            HIP_TRY(launch_weights_few(tab, g, qp, lse + head0, rt, to, st));
+        } else {
+            HIP_TRY(launch_weights_queries(g, qp, lse + head0, rt, ws + kTableBytes, (float2*)(ws + w.off_factors), st));
+            HIP_TRY(launch_weights(tab, g, ws + kTableBytes, (const float2*)(ws + w.off_factors), rt, (float*)(ws + w.off_parts), to, st));
+        }
+    }
+    return FREQKV_OK;
+}
+
+freqkv_status_t freqkv_evict(void* k, void* v, const float* weights, float* weights_out, int32_t* kept, const freqkv_layout_t* layout, int n_heads,
+                             int head_dim, int cur_len, int n_sink, int n_recent, int keep, const int32_t* cur_lens, int32_t* new_lens, void* stream)
+{
+    g_last_error[0] = 0;
+    if (!layout || (layout->dtype != FREQKV_BF16 && layout->dtype != FREQKV_F32) || n_heads < 1 || head_dim < 8) return FREQKV_E_INVALID;
+    if (!good_layout(layout, 8, head_dim)) return FREQKV_E_INVALID;
+    if (head_dim % 8) return FREQKV_E_UNSUPPORTED;
+    if (cur_len < 1 || cur_len > layout->token_capacity || n_sink < 0 || n_recent < 0 || keep < 1) return FREQKV_E_INVALID;
+    if (!weights || !kept || (((uintptr_t)weights | (uintptr_t)weights_out | (uintptr_t)kept | (uintptr_t)cur_lens | (uintptr_t)new_lens) & 3)) return FREQKV_E_INVALID;
+    if (new_lens && new_lens == cur_lens) return FREQKV_E_INVALID;            // (read again by the second kernel)
+    const freqkv_layout_t& L = *layout;
+    const int elem = L.dtype == FREQKV_BF16 ? 2 : 4;
+    std::vector<char*> bases;
+    if (!layer_bases(k, v, L, elem, &bases)) return FREQKV_E_INVALID;
+    EvictGeom g;
+    memset(&g, 0, sizeof(g));
+    g.row_bytes = head_dim * elem;
+    g.row_pieces = g.row_bytes / 16;
+    const int upl = L.batch * n_heads;
+    const long long units = (long long)std::min(L.n_layers, kLayersPerPass) * L.batch * n_heads;
+    if (units >= 1 << 20 || (long long)cur_len * g.row_pieces >= 1LL << 31) return FREQKV_E_UNSUPPORTED;
+    // slices of 64 bytes or more of a row, until there are two workgroups to a compute unit
+    g.slices = 1;
+    while (2 * units * g.slices < 512 && g.row_pieces % (2 * g.slices) == 0 && g.row_pieces / (2 * g.slices) >= 4) g.slices *= 2;
+    g.slice_pieces = g.row_pieces / g.slices;
+    g.n_kv = n_heads; g.units_per_layer = upl;
+    g.cur_len = cur_len; g.n_sink = n_sink; g.n_recent = n_recent; g.keep = keep; g.cur_lens = cur_lens; g.capacity = L.token_capacity;
+    g.by_layer = divisor(upl); g.by_kv = divisor(n_heads); g.by_slice = divisor(g.slices); g.by_pieces = divisor(g.slice_pieces);
+    g.stride_batch = L.stride_batch * elem; g.stride_head = L.stride_head * elem; g.stride_token = L.stride_token * elem;
+    const bool due = cur_lens || (long long)cur_len - n_sink - n_recent > keep;
+    for (int l0 = 0; l0 < L.n_layers; l0 += kLayersPerPass) {
+        const int layers = std::min(L.n_layers - l0, kLayersPerPass);
+        SlabTable tab;
+        slabs_of(bases, l0, layers, &tab);
+        g.units = layers * upl;
+        const long long u0 = (long long)l0 * upl;
+        int32_t* const to = kept + u0 * keep;
+        HIP_TRY(launch_evict_select(g, weights + u0 * L.token_capacity, weights_out ? weights_out + u0 * L.token_capacity : nullptr, to, new_lens, (hipStream_t)stream));
+        if (due) HIP_TRY(launch_evict_move(tab, g, to, (hipStream_t)stream));
     }
     return FREQKV_OK;
 }

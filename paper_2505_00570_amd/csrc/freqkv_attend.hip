@@ -18,32 +18,17 @@
 //   k_attend_quads    the same for groups of four query heads.
 //   k_attend_merge    combines the per-chunk states of a query head and writes the output row (not needed for one chunk).
 #include "freqkv_internal.h"
+#include "freqkv_lanes.h"
 
 namespace freqkv {
 
 namespace {
-
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 4;
 constexpr int kUnroll = 2;          // rows in flight per lane group per loop step (times two: prefetch)
 constexpr float kMinusBig = -1.0e30f;
 constexpr int kReseed = 32;          // loop steps between exact recomputations of the row cos/sin
 constexpr float kSlack = 8.0f;      // log2 of the largest un-rescaled softmax weight
-
-template <int I> struct IC { static constexpr int value = I; };
-template <int N, int I = 0, class F>
-__device__ __forceinline__ void static_for(F&& f)
-{
-    if constexpr (I < N) {
-        f(IC<I>{});
-        static_for<N, I + 1>(f);
-    }
-}
 
 // ---- P consecutive channels (P = 4 or 8), as stored and as floats ---------------------------------
 template <typename T, int P> struct Raw;
@@ -111,13 +96,6 @@ __device__ __forceinline__ void swap_halves(Raw<float, 8>& x, Raw<float, 8>& y)
     swap_halves(x.b, y.b);
 }
 
-__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
-
-// Lane exchange inside a row of 16 lanes through the data-parallel primitives (no LDS traffic).
-template <int CTRL> __device__ __forceinline__ float dpp(float x)
-{
-    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
-}
 // Sum over the LPR (4, 8, 16 or 32) adjacent lanes that share a cache row; every lane gets the sum.
 template <int LPR> __device__ __forceinline__ float group_sum(float x)
 {
@@ -129,35 +107,9 @@ template <int LPR> __device__ __forceinline__ float group_sum(float x)
     return x;
 }
 
-// Barrier for what the workgroup keeps in LDS.  (The other one would wait for all loads as well, those of rows past the end of a chunk among
-// them, which nobody uses: 2000 cycles at the end of every workgroup.)
-__device__ __forceinline__ void lds_barrier()
-{
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
-}
-
 // Lane I of each quad, in all four lanes of it.
 template <int I> __device__ __forceinline__ float quad_lane(float x) { return dpp<I * 0x55>(x); }
 
-// x op (x of the lane O further or nearer), in every lane; O = 4, 8, 16 or 32.  On the vector units: a shuffle goes through LDS, and
-// a chain of them is what the end of a short call waits for.
-template <int O, class F> __device__ __forceinline__ float fold(float x, F&& op)
-{
-    if constexpr (O == 4) {
-        return op(x, dpp<0x141>(dpp<0x1B>(x)));  // mirrored in the quad [3,2,1,0], then in the half row
-    } else if constexpr (O == 8) {
-        return op(x, dpp<0x128>(x));             // the row of 16 turned by 8
-    } else if constexpr (O == 16) {
-        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-        return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
-    } else {
-        static_assert(O == 32);
-        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-        return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
-    }
-}
 // Sums of two values over lanes O apart: the lanes without O in their index get that of x, the others that of y.
 template <int O> __device__ __forceinline__ float fold_two(float x, float y, [[maybe_unused]] int lane)
 {
@@ -190,24 +142,6 @@ template <int O> __device__ __forceinline__ Pair both(float x)
                      __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(i, i, 0x100 + O, 0xf, 0xf ^ upper, false))}};
     }
 }
-// ... over the lanes O, 2 O, ... 32 apart
-template <int O, class F> __device__ __forceinline__ float fold_from(float x, F&& op)
-{
-    x = fold<O>(x, op);
-    if constexpr (O < 32) x = fold_from<2 * O>(x, op);
-    return x;
-}
-// ... over all 64 lanes
-template <class F> __device__ __forceinline__ float wave_fold(float x, F&& op)
-{
-    x = op(x, dpp<0xB1>(x));                     // lanes 1, 2 and 4 apart (quads exchange halves, half rows of 8 mirror)
-    x = op(x, dpp<0x4E>(x));
-    x = op(x, dpp<0x141>(x));
-    return fold_from<8>(x, op);
-}
-struct Add { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
-struct Max { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
-
 // Four heads: the score of the row lane / (D / 16) and the head that the lane's place in its quad names, from the products of four rows with the
 // channels of its quad.  All quads that share a row get the same bits: where each keeps what it has, two lanes add up the same two
 // values.  (D = 256, with S0..S3 the sums of the quads of 16 lanes: turned by 8 first S0 + S2 and S1 + S3.  By 4 first, they would have
@@ -224,14 +158,6 @@ template <int D> __device__ __forceinline__ float row_score(f32x4 x, int lane)
         return t + dpp<0x124>(t);
     }
 }
-
-// Two adjacent results, rounded once.
-__device__ __forceinline__ void store2(uint16_t* p, float a, float b)
-{
-    f32x2 v = {a, b};
-    *(uint32_t*)p = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
-}
-__device__ __forceinline__ void store2(float* p, float a, float b) { *(f32x2*)p = f32x2{a, b}; }
 
 // cos and sin of pos * theta.  The product, its reduction to [-pi/4, pi/4] plus a quadrant and the two
 // short Taylor sums (truncation below 2e-9 on that interval) are all in fp64; the results are rounded once.
@@ -294,22 +220,6 @@ __device__ __forceinline__ int lane_index()
     uint32_t none = 0;
     asm volatile("" : "+v"(none));
     return __builtin_amdgcn_mbcnt_hi(~0u, __builtin_amdgcn_mbcnt_lo(~0u, none));
-}
-
-// Workgroups that read the same rows, for query heads beyond those of one, follow each other on one XCD (they are dealt round-robin to 8) and
-// find them in its L2 (8 query heads to each of 4 KV heads x 8192 rows x 32 layers 181 -> 159 us, of 8 x 4000 x 32 167 -> 155; with all
-// first parts ahead of all second ones, rows came from memory again).
-__device__ __forceinline__ void share_out(int parts, int& chunk_id, int& part)
-{
-    const int chunks = (int)gridDim.x / parts, whole = chunks & ~7, at = chunk_id - whole * parts;
-    if (at < 0) {
-        const int grp = chunk_id / (8 * parts), local = chunk_id - grp * 8 * parts;
-        part = local >> 3;
-        chunk_id = grp * 8 + (local & 7);
-    } else {
-        part = at / (chunks - whole);
-        chunk_id = whole + at - part * (chunks - whole);
-    }
 }
 
 // The end of a chunk, from the states of its lane groups in LDS (red: HSLOTS of them; largest scores and sums of each wave): sums, and the chunk's
@@ -1015,7 +925,8 @@ void k_attend_merge(const AttGeom, const float* __restrict__ part_acc, const flo
     __syncthreads();
     if (part == 0) {
         static_for<kMergeShare - 1>([&](auto i) { sum[0] += sh_sum[i.value + 1][pr][0]; sum[1] += sh_sum[i.value + 1][pr][1]; });
-        store2(out + head * D + 2 * pr, sum[0] / L, sum[1] / L);
+        // (a query that saw no row, which only calls over 8-bit caches have, is zero, and its lse -inf)
+        store2(out + head * D + 2 * pr, L == 0.f ? 0.f : sum[0] / L, L == 0.f ? 0.f : sum[1] / L);
         if (lse && pr == 0) lse[head] = 0.6931471805599453f * (M + log2f(L));
     }
 }

@@ -325,4 +325,107 @@ inline bool prefill_direct_fits(int cur_len, long long stride_token)
 hipError_t launch_attend_prefill(const PrefillGeom& g, const SlabTable* tab, const _Float16* Kr, const _Float16* Vt, const void* q, const float2* cs,
                                  void* out, float* lse, float* part_acc, float2* part_ml, hipStream_t st);
 
+// ---- 8-bit caches: codes with a scale for each block of tokens of a head --------------------------------
+enum Q8Format { kInt8 = 0, kE4M3 = 1 };
+
+// Rows that become codes, or codes that become rows (by-value kernel argument).  A slab is K or V of a layer; strides of rows and codes in bytes,
+// of scales in elements.
+struct Q8MoveGeom {
+    int format, elem_bytes;            // of the codes; of the rows (2 bfloat16, 4 float32)
+    int d, block_shift;                // head_dim, a multiple of 16; log2 of the tokens of a block
+    int n_heads, hts;                  // hts = batch * n_heads
+    int n_rows;
+    int row;                           // first of the rows
+    int code_row;                      // first of the codes' rows ...
+    const int* code_rows;              // ... or of each sequence's, a device array [batch] (quantise only)
+    int capacity;                      // of the codes' rows
+    int n_blk;                         // workgroups per head-tensor
+    Divisor by_blk, by_heads, by_pieces;   // n_blk, n_heads, pieces of a row that a thread handles
+    long long stride_batch, stride_head, stride_token;
+    long long code_batch, code_head, code_token;
+    long long scale_layer, scale_batch, scale_head;
+    float *k_scale, *v_scale;          // of the pass's first layer
+};
+hipError_t launch_quantize(const SlabTable& rows, const SlabTable& codes, const Q8MoveGeom& g, int slabs, hipStream_t st);
+constexpr int kDequantPieces = 4, kDequantPerWg = 256 * kDequantPieces;   // pieces of 16 codes: of a thread, of a workgroup
+hipError_t launch_dequantize(const SlabTable& codes, const SlabTable& rows, const Q8MoveGeom& g, int slabs, hipStream_t st);
+
+// Angles of the d / 2 rotary pairs: frequencies in quarter turns per row, the rotation that advances a position by kTurnStep rows, and the angles of the rows
+// 0 .. kTurnRows - 1, which turn the seed of a tile's first row into those of all its rows.
+constexpr int kTurnStep = 64, kTurnRows = 32;
+struct TurnTable {
+    const double* quarters;            // [d / 2]
+    const float2* step;                // [d / 2] (cos, sin)
+    const float2* rows;                // [kTurnRows][d / 2]
+};
+constexpr size_t turn_table_bytes(int d) { return (size_t)(d / 2) * (2 + kTurnRows) * 8; }
+inline TurnTable turn_table(const void* at, int d)
+{
+    const char* p = (const char*)at;
+    return TurnTable{(const double*)p, (const float2*)(p + d * 4), (const float2*)(p + d * 8)};
+}
+hipError_t launch_turn_table(void* at, int d, double base, hipStream_t st);
+
+// Attention over codes.  A unit is one (layer, sequence, KV head); its queries are the G heads that share it, q_len of each.
+constexpr int kQ8Waves = 4, kQ8Queries = 16;                           // waves of a workgroup, queries that it handles together
+constexpr int kQ8StepRows = 2 * kTurnStep;                             // rows of a workgroup's step: two tiles of each wave, kTurnStep rows apart
+static_assert(kTurnStep == 16 * kQ8Waves, "tiles of 16 rows");
+struct Q8AttGeom {
+    int format, f32;                   // of the codes; queries and results are float32 (else bfloat16)
+    int d, M, q_len;                   // M = G * q_len
+    int parts;                         // ceil(M / kQ8Queries)
+    int n_kv, units, units_per_layer;
+    int cur_len;                       // rows of a sequence (with cur_lens: of the longest)
+    const int* cur_lens;               // optional device array [batch]
+    int block_shift;
+    int n_split, chunk;                // chunks of a unit's rows; rows of one, a multiple of kQ8StepRows
+    Divisor by_split, by_layer, by_kv, by_q;
+    long long code_batch, code_head, code_token;
+    long long scale_layer, scale_batch, scale_head;
+    const float *k_scale, *v_scale;    // of the pass's first layer
+    float qscale;                      // log2(e) / sqrt(d)
+};
+hipError_t launch_attend_q8(const SlabTable& tab, const Q8AttGeom& g, const void* q, const TurnTable& rt, float* part_acc, float* part_ml, void* out,
+                            float* lse, hipStream_t st);
+
+// ---- attention weights of the cached rows, and eviction by them -----------------------------------------
+constexpr int kWeightFew = 16;         // queries of a unit that k_weights_few takes
+constexpr int kWeightTile = 32;        // k_weights: queries of a tile, keys of a wave
+constexpr int kWeightKeys = 128;       // ... keys of a workgroup
+struct WeightGeom {
+    int elem_bytes, d, M, q_len;       // M = queries of a unit: heads that share a KV head, q_len of each
+    int n_kv, units, units_per_layer;
+    int cur_len;
+    const int* cur_lens;               // optional device array [batch]
+    int accumulate;
+    int capacity;                      // rows of `weights`
+    int n_chunk, chunk;                // k_weights_few: chunks of a unit's rows (chunk a multiple of kTurnStep)
+    int q_tiles, n_split, split_tiles; // k_weights: tiles of a unit's queries; parts of them, of split_tiles tiles each
+    int key_blocks;                    // ... workgroups over a unit's rows
+    Divisor by_chunk, by_layer, by_kv, by_q, by_keys, by_split;
+    long long stride_batch, stride_head, stride_token;   // elements
+    float qscale;                      // log2(e) / sqrt(d)
+};
+// operands: [unit][q_tiles][hi, lo][d / 16][64 lanes][8] fp16; factors: [unit][q_tiles][32] (factor of a score, -log2(e) lse)
+inline size_t weight_operand_bytes(int d) { return (size_t)kWeightTile * d * 4; }
+hipError_t launch_weights_few(const SlabTable& tab, const WeightGeom& g, const void* q, const float* lse, const TurnTable& rt, float* weights, hipStream_t st);
+hipError_t launch_weights_queries(const WeightGeom& g, const void* q, const float* lse, const TurnTable& rt, void* operands, float2* factors, hipStream_t st);
+// parts: [n_split][units][cur_len] where n_split > 1
+hipError_t launch_weights(const SlabTable& tab, const WeightGeom& g, const void* operands, const float2* factors, const TurnTable& rt, float* parts,
+                          float* weights, hipStream_t st);
+
+struct EvictGeom {
+    int row_bytes, row_pieces;         // of a head's row; in pieces of 16 bytes
+    int slices, slice_pieces;          // a workgroup moves slice_pieces pieces of every row
+    int n_kv, units, units_per_layer;
+    int cur_len, n_sink, n_recent, keep;
+    const int* cur_lens;               // optional device array [batch]
+    int capacity;                      // rows of `weights`
+    Divisor by_layer, by_kv, by_slice, by_pieces;
+    long long stride_batch, stride_head, stride_token;   // bytes
+};
+// new_lens: of the whole batch, written by the first layer's units (first_layer)
+hipError_t launch_evict_select(const EvictGeom& g, const float* weights, float* weights_out, int* kept, int* new_lens, hipStream_t st);
+hipError_t launch_evict_move(const SlabTable& tab, const EvictGeom& g, const int* kept, hipStream_t st);
+
 }  // namespace freqkv
