@@ -408,8 +408,8 @@ FREQKV_API freqkv_status_t freqkv_attend_q8_plan(const freqkv_layout_t* layout8,
  *   cur_lens  optional DEVICE array [batch] of int32: cached rows of each sequence, clamped to [0, cur_len]; cur_len is then their upper bound.  Queries
  *             that sit ahead of row 0 (n < q_len) see nothing: their results are zero, their lse -inf.  Rows at and beyond a sequence's length are not read.
  *   layout8.workspace  freqkv_attend_q8_plan(...).workspace_bytes, 256-byte aligned; with less the rows are cut into fewer chunks, down to one
- * head_dim 64, 128 or 256.  Operands of the matrix cores are fp16, exact for the codes, 11 bits for turned keys, queries and softmax weights; with
- * q_dtype FREQKV_F32 each is a sum of two, 22 bits.  Sums are fp32.  Queries and scales may have any finite magnitude.  q, out and lse must be 16-byte aligned.
+ * head_dim 64, 128 or 256.  Operands of the matrix cores are fp16, exact for the codes, 11 bits for turned keys, queries and softmax weights, in chunks of many queries for values
+ * as well; with q_dtype FREQKV_F32 each is a sum of two, 22 bits.  Sums are fp32.  Queries and scales may have any finite magnitude.  q, out and lse must be 16-byte aligned.
  */
 FREQKV_API freqkv_status_t freqkv_attend_q8(const void* q, const void* k8, const void* v8, void* out, float* lse, const freqkv_layout_t* layout8,
                                  const freqkv_scales_t* scales, int q_dtype, int n_q_heads, int n_kv_heads, int head_dim, int cur_len, int q_len,
@@ -481,6 +481,8 @@ FREQKV_API freqkv_status_t freqkv_debug_fast_stage(void* k, void* v, const freqk
  *       workspace of workspace_bytes allows (FREQKV_E_WORKSPACE: too small for the call); of k_attend_prefill, whether the call goes there or not
  *   freqkv_debug_prefill_kernel   a static string: "k_attend_prefill (operands)", after the pass that writes them, "k_attend_prefill (rows)", on the
  *       cached rows, or "k_attend_quads", few queries as heads of a decode call; NULL for calls that are refused
+ *   freqkv_debug_attend_q8_kernel   the same of freqkv_attend_q8 with the workspace that its plan asks for: "k_attend_q8" or "k_attend_prefill (operands
+ *       of codes)"; ragged: the call has cur_lens
  */
 FREQKV_API const char* freqkv_debug_compress_kernel(const freqkv_layout_t* layout, int n_heads, int head_dim, int window, int n_sink,
                                          double retain_ratio);
@@ -492,6 +494,9 @@ FREQKV_API freqkv_status_t freqkv_debug_prefill_cut(const freqkv_layout_t* layou
                                          int32_t* parts /* host */);
 FREQKV_API const char* freqkv_debug_prefill_kernel(const freqkv_layout_t* layout, int n_q_heads, int n_kv_heads, int head_dim,
                                          int cur_len, int q_len, size_t workspace_bytes);
+
+FREQKV_API const char* freqkv_debug_attend_q8_kernel(const freqkv_layout_t* layout8, int q_dtype, int n_q_heads, int n_kv_heads, int head_dim,
+                                         int cur_len, int q_len, int ragged);
 
 /* Human-readable name of a status code (static string, host). */
 FREQKV_API const char* freqkv_status_string(freqkv_status_t status);

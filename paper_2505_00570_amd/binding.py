@@ -138,6 +138,8 @@ def load() -> C.CDLL:
     lib.freqkv_attend_weights_plan.argtypes = [LP, ci, ci, ci, ci, ci, C.POINTER(AttendPlan)]
     lib.freqkv_attend_weights.argtypes = [vp, vp, vp, vp, LP, ci, ci, ci, ci, ci, vp, ci, C.c_double, vp]
     lib.freqkv_evict.argtypes = [vp, vp, vp, vp, vp, LP, ci, ci, ci, ci, ci, ci, vp, vp, vp]
+    lib.freqkv_debug_attend_q8_kernel.argtypes = [LP, ci, ci, ci, ci, ci, ci, ci]
+    lib.freqkv_debug_attend_q8_kernel.restype = C.c_char_p
     for name in ("quantize", "dequantize", "attend_q8_plan", "attend_q8", "attend_weights_plan", "attend_weights", "evict"):
         getattr(lib, "freqkv_" + name).restype = C.c_int
     lib.freqkv_prepare.argtypes = [C.c_int, C.c_uint32, C.c_int, C.c_int, C.c_double, C.c_void_p]
@@ -364,6 +366,14 @@ def attend_q8(q, k8, v8, out, lse, layout8: Layout, scales: Scales, q_dtype: int
                                  C.byref(scales), q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, _dev_ptr(cur_lens),
                                  float(rope_base), _stream_ptr(stream))
     return _check(rc) if check else rc
+
+
+def attend_q8_kernel(layout8: Layout, q_dtype: int, n_q_heads: int, n_kv_heads: int, head_dim: int, cur_len: int, q_len: int = 1,
+                     ragged: bool = False):
+    """freqkv_debug_attend_q8_kernel: the way such a call takes with the workspace that its plan asks for; None where it is refused."""
+    name = load().freqkv_debug_attend_q8_kernel(C.byref(layout8), q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len,
+                                                1 if ragged else 0)
+    return name.decode() if name is not None else None
 
 
 def attend_weights_plan(layout: Layout, n_q_heads: int, n_kv_heads: int, head_dim: int, cur_len: int, q_len: int = 1,

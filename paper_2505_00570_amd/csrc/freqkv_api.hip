@@ -1795,6 +1795,12 @@ freqkv_status_t q8_move(bool quantize, const void* k, const void* v, const freqk
     return FREQKV_OK;
 }
 
+// Whether operands written first are faster than k_attend_q8, which reads rows once for 16 queries.
+bool q8_prefill_pays(const PrefillShape& p)
+{
+    return p.a.G * p.q_len > 64;
+}
+
 struct Q8Shape {
     long long units_all, units;         // all; of a pass
     int M, parts, n_split, chunk;
@@ -1829,6 +1835,59 @@ freqkv_status_t check_q8(const freqkv_layout_t* L, int q_dtype, int n_q, int n_k
     s.cut(std::min(most, std::max(1LL, 512 / (s.units * s.parts))), cur_len, d);
     if (s.units * s.n_split >= 1 << 23) return FREQKV_E_UNSUPPORTED;
     *out = s;
+    return FREQKV_OK;
+}
+
+// A chunk of many queries of bf16 over codes of 128 channels goes as over a bf16 cache, operands written first (the powers of two lie ahead of that way's workspace).
+bool q8_as_prefill(const freqkv_layout_t& L, int q_dtype, int n_q, int n_kv, int d, int cur_len, int q_len, bool ragged, PrefillShape* p)
+{
+    if (q_dtype != FREQKV_BF16 || d != 128 || ragged || q_len < 2) return false;
+    freqkv_layout_t rows = L;
+    rows.dtype = FREQKV_BF16;
+    if (check_prefill(&rows, n_q, n_kv, d, cur_len, q_len, p) != FREQKV_OK) return false;
+    return q8_prefill_pays(*p);
+}
+size_t powers_bytes(const PrefillShape& p) { return (size_t)round_up(p.units * (long long)sizeof(float2), 256); }
+
+freqkv_status_t attend_q8_prefill(const PrefillShape& p, int split_tiles, const std::vector<char*>& bases, const void* q, void* out, float* lse,
+                                  const freqkv_layout_t& L, const freqkv_scales_t& scales, int shift, double rope_base, hipStream_t st)
+{
+    const AttShape& a = p.a;
+    char* const powers = (char*)L.workspace;
+    char* const ws = powers + powers_bytes(p);
+    const float2* cs = nullptr;
+    freqkv_status_t rc = get_cs_table(a.cur_len, a.d, rope_base, st, (float2*)ws, &cs);
+    if (rc < 0) return rc;
+    const int upl = a.batch * a.n_kv;
+    for (int l0 = 0; l0 < a.n_layers; l0 += p.layers_per_pass) {
+        const int layers = std::min(a.n_layers - l0, p.layers_per_pass);
+        SlabTable tab;
+        slabs_of(bases, l0, layers, &tab);
+        PrefillGeom g;
+        memset(&g, 0, sizeof(g));
+        g.d = a.d; g.G = a.G; g.n_kv = a.n_kv;
+        g.units = layers * upl; g.units_per_layer = upl;
+        g.cur_len = a.cur_len; g.q_len = p.q_len; g.q_pad = p.q_pad; g.q_blocks = p.q_pad / 32;
+        g.key_tiles = p.key_tiles; g.n_split = p.n_split; g.split_tiles = split_tiles; g.halves = p.halves;
+        g.stride_batch = L.stride_batch; g.stride_head = L.stride_head; g.stride_token = L.stride_token;
+        g.qscale = (float)(1.4426950408889634 / std::sqrt((double)a.d));
+        const Codes8 codes = {q8_format(L), shift, scales.stride_layer, scales.stride_batch, scales.stride_head, scales.k + l0 * scales.stride_layer,
+                              scales.v + l0 * scales.stride_layer};
+        const long long head0 = (long long)l0 * upl * a.G;
+        const char* qp = (const char*)q + head0 * p.q_len * a.d * 2;
+        char* op = (char*)out + head0 * p.q_len * a.d * 2;
+        _Float16 *const kr = (_Float16*)(ws + p.off_kr), *const vt = (_Float16*)(ws + p.off_vt);
+        ProfSpan sp;
+        HIP_TRY(prof_begin(st, 0, &sp));
+        HIP_TRY(launch_prefill_prepare8(tab, g, codes, cs, kr, vt, (float2*)powers, st));
+        HIP_TRY(prof_end(st, &sp));
+        HIP_TRY(prof_begin(st, 3, &sp));
+        const long long tasks = (long long)g.units * a.G * g.q_blocks;
+        float* part_acc = p.n_split > 1 ? (float*)(ws + p.off_part) : nullptr;
+        float2* part_ml = p.n_split > 1 ? (float2*)(part_acc + tasks * p.n_split * 32 * a.d) : nullptr;
+        HIP_TRY(launch_attend_prefill(g, nullptr, kr, vt, qp, cs, op, lse ? lse + head0 * p.q_len : nullptr, part_acc, part_ml, st, (const float2*)powers));
+        HIP_TRY(prof_end(st, &sp));
+    }
     return FREQKV_OK;
 }
 
@@ -1897,6 +1956,9 @@ freqkv_status_t freqkv_attend_q8_plan(const freqkv_layout_t* layout8, int q_dtyp
     out->chunk_rows = s.chunk;
     out->heads_together = std::min(s.M, kQ8Queries);
     out->workspace_bytes = s.workspace_bytes;
+    PrefillShape p;
+    if (q8_as_prefill(*layout8, q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, false, &p))
+        out->workspace_bytes = std::max(out->workspace_bytes, p.workspace_bytes + powers_bytes(p));
     const double seen = (double)q_len * (cur_len - q_len) + 0.5 * (double)q_len * (q_len + 1);
     const double e = q_dtype == FREQKV_BF16 ? 2.0 : 4.0;
     out->bytes_algorithmic = (double)s.units_all * (2.0 * cur_len * head_dim + 2.0 * s.M * head_dim * e);
@@ -1919,9 +1981,15 @@ freqkv_status_t freqkv_attend_q8(const void* q, const void* k8, const void* v8, 
     const freqkv_layout_t& L = *layout8;
     std::vector<char*> bases;
     if (!layer_bases(k8, v8, L, 1, &bases)) return FREQKV_E_INVALID;
+    if (!L.workspace || ((uintptr_t)L.workspace & 255)) return FREQKV_E_WORKSPACE;
+    PrefillShape p;
+    int split_tiles = 0;
+    if (q8_as_prefill(L, q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, cur_lens != nullptr, &p) && L.workspace_bytes >= powers_bytes(p) &&
+        fit_prefill(&p, L.workspace_bytes - powers_bytes(p), &split_tiles) == FREQKV_OK)
+        return attend_q8_prefill(p, split_tiles, bases, q, out, lse, L, *scales, shift, rope_base, (hipStream_t)stream);
     // (a workspace planned at another length: fewer chunks)
     while (s.n_split > 1 && s.workspace_bytes > L.workspace_bytes) s.cut(s.n_split - 1, cur_len, head_dim);
-    if (!L.workspace || ((uintptr_t)L.workspace & 255) || L.workspace_bytes < s.workspace_bytes) return FREQKV_E_WORKSPACE;
+    if (L.workspace_bytes < s.workspace_bytes) return FREQKV_E_WORKSPACE;
     char* const ws = (char*)L.workspace;
     hipStream_t st = (hipStream_t)stream;
     RopeEntry* rt = nullptr;
@@ -1963,6 +2031,15 @@ freqkv_status_t freqkv_attend_q8(const void* q, const void* k8, const void* v8, 
         HIP_TRY(launch_attend_merge(m, elem, pa, pm, op, ls, st));
     }
     return FREQKV_OK;
+}
+
+const char* freqkv_debug_attend_q8_kernel(const freqkv_layout_t* layout8, int q_dtype, int n_q_heads, int n_kv_heads, int head_dim, int cur_len, int q_len,
+                                          int ragged)
+{
+    Q8Shape s;
+    PrefillShape p;
+    if (check_q8(layout8, q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, &s) < 0) return nullptr;
+    return q8_as_prefill(*layout8, q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, ragged != 0, &p) ? "k_attend_prefill (operands of codes)" : "k_attend_q8";
 }
 
 freqkv_status_t freqkv_attend_weights_plan(const freqkv_layout_t* layout, int n_q_heads, int n_kv_heads, int head_dim, int cur_len, int q_len,

@@ -323,10 +323,19 @@ inline bool prefill_direct_fits(int cur_len, long long stride_token)
 // q: dense [units*G][q_len][d] bf16, rotated inside the attention kernel.  part_acc, part_ml (n_split > 1): per (task, part)
 // 32 x d fp32 and 32 x (reference point, sum).
 hipError_t launch_attend_prefill(const PrefillGeom& g, const SlabTable* tab, const _Float16* Kr, const _Float16* Vt, const void* q, const float2* cs,
-                                 void* out, float* lse, float* part_acc, float2* part_ml, hipStream_t st);
+                                 void* out, float* lse, float* part_acc, float2* part_ml, hipStream_t st, const float2* powers = nullptr);
 
 // ---- 8-bit caches: codes with a scale for each block of tokens of a head --------------------------------
 enum Q8Format { kInt8 = 0, kE4M3 = 1 };
+
+// Operands of chunk-wise attention from codes (PrefillGeom's strides then are the codes', in bytes), and the powers of two that each unit's are divided by.
+struct Codes8 {
+    int format, block_shift;
+    long long scale_layer, scale_batch, scale_head;
+    const float *k_scale, *v_scale;    // of the pass's first layer
+};
+hipError_t launch_prefill_prepare8(const SlabTable& tab, const PrefillGeom& g, const Codes8& codes, const float2* cs, _Float16* Kr, _Float16* Vt, float2* powers,
+                                   hipStream_t st);
 
 // Rows that become codes, or codes that become rows (by-value kernel argument).  A slab is K or V of a layer; strides of rows and codes in bytes,
 // of scales in elements.

@@ -21,6 +21,8 @@
 // rows and makes the tiles of them itself, in LDS.
 #include "freqkv_internal.h"
 
+#include <type_traits>
+
 namespace freqkv {
 
 namespace {
@@ -66,9 +68,22 @@ __device__ __forceinline__ half2v pack_half2(float a, float b)
 // the kernel's first arguments: behind all others they came 0.1 us later (365 queries over 365 rows of 8 KV heads 14.40 -> 14.49 us, 335 over 4 x 4 x 335 14.07 -> 14.20).
 template <bool DIRECT> struct Rows { void* none; };
 template <> struct Rows<true> { SlabTable tab; };
+// POWERS: operands that k_prefill_prep8 wrote, of codes; each unit's keys and values are divided by these.
+struct Powers { const float2* of_unit; };
 
 // Workgroups of k_prefill_prep to a unit, some of which may have no tile.
 __host__ __device__ inline int prep_tiles(int key_tiles) { return key_tiles < 64 || (-key_tiles & 7) * 14 > key_tiles ? key_tiles : (key_tiles + 7) & ~7; }
+
+// Values of four codes of one byte.
+template <int FMT> __device__ __forceinline__ void code_values(uint32_t w, float (&x)[4])
+{
+    if constexpr (FMT == kInt8) {
+        static_for<4>([&](auto i) { x[i.value] = (float)(int)(signed char)(w >> 8 * i.value); });
+    } else {
+        const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), b = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+        x[0] = a[0]; x[1] = a[1]; x[2] = b[0]; x[3] = b[1];
+    }
+}
 
 // Position of the key that sits at storage index s (0..31) of a Vt tile: the matrix core leaves a
 // 32x32 result with register r of a lane in half-wave hw at row 8*(r/4) + 4*hw + r%4; k-step t of the
@@ -188,6 +203,104 @@ __global__ __launch_bounds__(256) void k_prefill_prep(const PrefillGeom, const f
     *(half8*)(dst + 8) = hiv;
 }
 
+// The same operands of a cache held in 8 bits (codes with a scale for each block of tokens of a head): a tile's rows are half as many bytes, a thread has 8 pairs of a
+// key as above and 16 bytes of a value's row.  Keys and values of a unit are divided by powers of two, which a workgroup gets from the largest of the unit's
+// scales (each for itself: some hundred floats from the L2): fp16 then holds them whatever their magnitude, keys up to 2^7, so that queries
+// times the power are about what they are over a bf16 cache, values up to 2^13.  A row whose scale of K or V is NaN has a NaN key and a zero value: scores make
+// NaN what sees it, and a weight of zero leaves alone what does not.
+template <int FMT>
+__global__ __launch_bounds__(256) void k_prefill_prep8(const PrefillGeom, const Codes8 s8, const float2* __restrict__ cs, _Float16* __restrict__ Kr, _Float16* __restrict__ Vt,
+                                                       float2* __restrict__ powers, const SlabTable tab)
+{
+    const PrefillGeom g = first_argument<decltype(k_prefill_prep8<FMT>)>();
+    __shared__ uint32_t sm[kKeyTile][kD / 2 + 1];             // [key][pair of channels], one word of padding per row
+    __shared__ float most[2][4];
+    constexpr int half = kD / 2, pgn = half / 8;
+    const int tiles = prep_tiles(g.key_tiles), tile = blockIdx.x % tiles, unit = blockIdx.x / tiles;      // (as in k_prefill_prep)
+    if (tile >= g.key_tiles) return;
+    const int layer = unit / g.units_per_layer;
+    const int rem = unit - layer * g.units_per_layer;
+    const int b = rem / g.n_kv, kvh = rem - b * g.n_kv;
+    const long long head = (long long)b * g.stride_batch + (long long)kvh * g.stride_head;
+    const char* khead = tab.base[2 * layer] + head;
+    const char* vhead = tab.base[2 * layer + 1] + head;
+    const long long shead = (long long)layer * s8.scale_layer + (long long)b * s8.scale_batch + (long long)kvh * s8.scale_head;
+    const float *ks = s8.k_scale + shead, *vs = s8.v_scale + shead;
+    const int key = threadIdx.x / pgn, pg = threadIdx.x % pgn, j0 = pg * 8;    // the thread's key piece; its value piece has the same row
+    const int row = tile * kKeyTile + key;
+    u32x2 lo = {0u, 0u}, up = lo;
+    u32x4 vw = {0u, 0u, 0u, 0u};                              // rows beyond cur_len are zero
+    f32x4 c[4] = {};
+    float kscale = 0.f, vscale = 0.f;
+    if (row < g.cur_len) {
+        const char* kr = khead + (long long)row * g.stride_token;
+        lo = *(const u32x2*)(kr + j0);
+        up = *(const u32x2*)(kr + half + j0);
+        vw = *(const u32x4*)(vhead + (long long)row * g.stride_token + pg * 16);
+        const f32x4* cr = (const f32x4*)(cs + (long long)row * half + j0);
+        static_for<4>([&](auto i) { c[i.value] = cr[i.value]; });
+        kscale = ks[row >> s8.block_shift];
+        vscale = vs[row >> s8.block_shift];
+    }
+    float mk = 0.f, mv = 0.f;
+    for (int i = threadIdx.x; i <= (g.cur_len - 1) >> s8.block_shift; i += 256) {
+        mk = fmaxf(mk, ks[i]);
+        mv = fmaxf(mv, vs[i]);
+    }
+    for (int o = 32; o; o >>= 1) {
+        mk = fmaxf(mk, __shfl_xor(mk, o));
+        mv = fmaxf(mv, __shfl_xor(mv, o));
+    }
+    if ((threadIdx.x & 63) == 0) { most[0][threadIdx.x >> 6] = mk; most[1][threadIdx.x >> 6] = mv; }
+    __syncthreads();
+    static_for<4>([&](auto w) { mk = fmaxf(mk, most[0][w.value]); mv = fmaxf(mv, most[1][w.value]); });
+    // 2^e <= scale < 2^(e + 1), codes up to 127 or 448
+    constexpr int bits = FMT == kInt8 ? 7 : 9;
+    auto power = [](float x, int to) { return x > 0.f && x < INFINITY ? max(-120, min((int)(__float_as_uint(x) >> 23) - 127 - to, 120)) : 0; };
+    const int ke = power(mk, 6 - bits), ve = power(mv, 12 - bits);
+    if (tile == 0 && threadIdx.x == 0) powers[unit] = float2{ldexpf(1.f, ke), ldexpf(1.f, ve)};
+    const bool bad = !(kscale < INFINITY) || !(vscale < INFINITY);
+    const float kf = bad ? __uint_as_float(0x7fc00000u) : kscale * ldexpf(1.f, -ke), vf = bad ? 0.f : vscale * ldexpf(1.f, -ve);
+    static_for<4>([&](auto w) {
+        float x[4];
+        code_values<FMT>(vw[w.value], x);
+        static_for<2>([&](auto n) { sm[key][pg * 8 + 2 * w.value + n.value] = __builtin_bit_cast(uint32_t, pack_half2(x[2 * n.value] * vf, x[2 * n.value + 1] * vf)); });
+    });
+    const long long tile0 = ((long long)unit * g.key_tiles + tile) * (kKeyTile * kD);
+    {
+        half8 lo8 = {}, up8 = {};
+        if (row < g.cur_len) {
+            static_for<2>([&](auto w) {
+                float a[4], bb[4];
+                code_values<FMT>(lo[w.value], a);
+                code_values<FMT>(up[w.value], bb);
+                static_for<4>([&](auto j) {
+                    constexpr int i = 4 * w.value + j.value;
+                    const float co = c[i / 2][i % 2 * 2] * kf, si = c[i / 2][i % 2 * 2 + 1] * kf;
+                    lo8[i] = (_Float16)(a[j.value] * co - bb[j.value] * si);
+                    up8[i] = (_Float16)(bb[j.value] * co + a[j.value] * si);
+                });
+            });
+        }
+        _Float16* dst = Kr + tile0 + ((long long)pg * kKeyTile + key) * 8;
+        *(half8*)dst = lo8;
+        *(half8*)(dst + pgn * kKeyTile * 8) = up8;
+    }
+    __syncthreads();
+    // thread = (k-step t, half-wave hw, pair of channels): two adjacent 16-byte groups of the tile
+    const int cp = threadIdx.x & 63, hw = (threadIdx.x >> 6) & 1, t = threadIdx.x >> 7;
+    half8 lov, hiv;
+    static_for<8>([&](auto e) {
+        const half2v w = __builtin_bit_cast(half2v, sm[vt_key(16 * t + 8 * hw + e.value)][cp]);
+        lov[e.value] = w[0];
+        hiv[e.value] = w[1];
+    });
+    const int ch = 2 * cp, db = ch >> 5, dl = ch & 31;
+    _Float16* dst = Vt + tile0 + (long long)(((db * 2 + t) * 2 + hw) * 32 + dl) * 8;
+    *(half8*)dst = lov;
+    *(half8*)(dst + 8) = hiv;
+}
+
 // Workgroup = 8 waves = 8 tasks of one KV unit, two waves per SIMD; a task is (query head of the KV group,
 // block of 32 queries), heads fastest, so that with 4 query heads per KV head the waves walk the same keys.
 // A wave keeps its 32 queries, their 128 x 32 output block and two 32 x 32 score blocks in vector registers
@@ -204,13 +317,14 @@ __global__ __launch_bounds__(256) void k_prefill_prep(const PrefillGeom, const f
 // 0.52 in halves.  (In halves cos and sin that turn on from key to key, from the table every eighth tile, made whole calls up to 9 % shorter, 128 queries over
 // 4 x 4 x 6431 rows 41.5 -> 37.8 us, but are up to 7e-7 off where the table's are 3e-8.)  Rows touched
 // ahead of time, so that they come from the L2, changed nothing.  prefill_direct says which calls gain by it.
-template <int HALVES, bool DIRECT>
+template <int HALVES, bool DIRECT, bool POWERS = false>
 __global__ __launch_bounds__(kPrefillWaves * 64, 2)
 void k_attend_prefill(const PrefillGeom, const _Float16* __restrict__ Kr, const _Float16* __restrict__ Vt,
                       const uint16_t* __restrict__ q, const float2* __restrict__ cs, uint16_t* __restrict__ out,
-                      float* __restrict__ lse, float* __restrict__ part_acc, float2* __restrict__ part_ml, const Rows<DIRECT> rows)
+                      float* __restrict__ lse, float* __restrict__ part_acc, float2* __restrict__ part_ml,
+                      const std::conditional_t<POWERS, Powers, Rows<DIRECT>> rows)
 {
-    const PrefillGeom g = first_argument<decltype(k_attend_prefill<HALVES, DIRECT>)>();
+    const PrefillGeom g = first_argument<decltype(k_attend_prefill<HALVES, DIRECT, POWERS>)>();
     constexpr int TASKS = kPrefillWaves / HALVES;                        // of a workgroup
     __shared__ __attribute__((aligned(1024))) char ring[HALVES][2][4][kTileBytes];   // of each half: Kr tiles t+1, t+2, t+3 of step t, Vt tiles t .. t+3
     constexpr int QUERIES = 32 * kD * 2, ORIGIN = HALVES == 1 ? (kD / 2) * 8 : 0;
@@ -280,6 +394,12 @@ void k_attend_prefill(const PrefillGeom, const _Float16* __restrict__ Kr, const 
         my_tiles = min(my_tiles, wg_tiles);
     }
     const bool seen = my_tiles > part0;                            // the task sees keys of this part
+    float qscale = g.qscale, vpower = 1.f;
+    if constexpr (POWERS) {
+        const float2 of_unit = rows.of_unit[unit];
+        qscale *= of_unit.x;
+        vpower = of_unit.y;
+    }
     // this half's tiles: t0 .. t0 + steps - 1, of which there may be one less for the second half
     const int steps = HALVES == 1 ? wg_tiles - part0 : (wg_tiles - part0 + 1) / 2;
     const int t0 = part0 + half * steps, t1 = min(t0 + steps, wg_tiles);
@@ -443,7 +563,7 @@ void k_attend_prefill(const PrefillGeom, const _Float16* __restrict__ Kr, const 
             *(u32x4*)(table + (row >> 4) * TABLE_HALF + (row & 15) * 512 + (rpiece ^ (row & 15)) * 16) = rt[i.value];
         });
         if (active) {
-            *(float2*)(origin + lane * 8) = {o.x * g.qscale, o.y * g.qscale};
+            *(float2*)(origin + lane * 8) = {o.x * qscale, o.y * qscale};
             static_for<NL>([&](auto j) {
                 const int row = 64 / NP * j.value + r0;
                 *(u32x4*)(turn + row * (NP * 16) + (pi ^ (HALVES == 1 ? row & 15 : row >> 1 & 7)) * 16) = x[j.value];
@@ -709,6 +829,7 @@ void k_attend_prefill(const PrefillGeom, const _Float16* __restrict__ Kr, const 
             });
         });
     }
+    if constexpr (POWERS) static_for<NB>([&](auto db) { static_for<16>([&](auto r) { fin[db.value][r.value] *= vpower; }); });
     if (g.n_split > 1) {
         // the state as it is, in the order of the registers (1 KB per store): [task][part][channel block][register / 4][lane][4]
         if (seen) {
@@ -829,12 +950,22 @@ hipError_t launch_prefill_prepare(const SlabTable& tab, const PrefillGeom& g, co
     return hipGetLastError();
 }
 
+hipError_t launch_prefill_prepare8(const SlabTable& tab, const PrefillGeom& g, const Codes8& codes, const float2* cs, _Float16* Kr, _Float16* Vt, float2* powers,
+                                   hipStream_t st)
+{
+    if (g.d != kD || g.cur_len < 1 || g.key_tiles * kKeyTile < g.cur_len) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)((long long)g.units * prep_tiles(g.key_tiles)));
+    if (codes.format == kInt8) hipLaunchKernelGGL(k_prefill_prep8<kInt8>, grid, dim3(256), 0, st, g, codes, cs, Kr, Vt, powers, tab);
+    else                       hipLaunchKernelGGL(k_prefill_prep8<kE4M3>, grid, dim3(256), 0, st, g, codes, cs, Kr, Vt, powers, tab);
+    return hipGetLastError();
+}
+
 hipError_t launch_attend_prefill(const PrefillGeom& g, const SlabTable* tab, const _Float16* Kr, const _Float16* Vt, const void* q, const float2* cs,
-                                 void* out, float* lse, float* part_acc, float2* part_ml, hipStream_t st)
+                                 void* out, float* lse, float* part_acc, float2* part_ml, hipStream_t st, const float2* powers)
 {
     if (g.d != kD || g.q_blocks * kQPerWave != g.q_pad) return hipErrorInvalidValue;
     if (g.halves != 1 && g.halves != 2) return hipErrorInvalidValue;
-    if (tab ? !prefill_direct_fits(g.cur_len, g.stride_token) : !Kr || !Vt) return hipErrorInvalidValue;
+    if (tab ? powers || !prefill_direct_fits(g.cur_len, g.stride_token) : !Kr || !Vt) return hipErrorInvalidValue;
     if (g.n_split < 1 || (g.n_split > 1 && (!part_acc || !part_ml || (long long)g.n_split * g.split_tiles < g.key_tiles))) return hipErrorInvalidValue;
     const int tasks = kPrefillWaves / g.halves, wgs_per_unit = (g.G * g.q_blocks + tasks - 1) / tasks;
     PrefillGeom gw = g;
@@ -844,7 +975,11 @@ hipError_t launch_attend_prefill(const PrefillGeom& g, const SlabTable* tab, con
     auto launch = [&](auto kernel, const auto& rows) {
         hipLaunchKernelGGL(kernel, grid, block, 0, st, gw, Kr, Vt, (const uint16_t*)q, cs, (uint16_t*)out, lse, part_acc, part_ml, rows);
     };
-    if (tab) {
+    if (powers) {
+        const Powers of = {powers};
+        if (g.halves == 2) launch(k_attend_prefill<2, false, true>, of);
+        else               launch(k_attend_prefill<1, false, true>, of);
+    } else if (tab) {
         const Rows<true> rows = {*tab};
         if (g.halves == 2) launch(k_attend_prefill<2, true>, rows);
         else               launch(k_attend_prefill<1, true>, rows);
