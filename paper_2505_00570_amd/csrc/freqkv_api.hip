@@ -2130,14 +2130,14 @@ freqkv_status_t freqkv_evict(void* k, void* v, const float* weights, float* weig
     g.row_pieces = g.row_bytes / 16;
     const int upl = L.batch * n_heads;
     const long long units = (long long)std::min(L.n_layers, kLayersPerPass) * L.batch * n_heads;
-    if (units >= 1 << 20 || (long long)cur_len * g.row_pieces >= 1LL << 31) return FREQKV_E_UNSUPPORTED;
-    // slices of 64 bytes or more of a row, until there are two workgroups to a compute unit
+    if (units >= 1 << 20 || (long long)cur_len * g.row_pieces >= 1LL << 30) return FREQKV_E_UNSUPPORTED;
+    // slices of a row, of 16 bytes or more, until there is a workgroup to each compute unit
     g.slices = 1;
-    while (2 * units * g.slices < 512 && g.row_pieces % (2 * g.slices) == 0 && g.row_pieces / (2 * g.slices) >= 4) g.slices *= 2;
+    while (2 * units * g.slices < 256 && g.row_pieces % (2 * g.slices) == 0) g.slices *= 2;
     g.slice_pieces = g.row_pieces / g.slices;
     g.n_kv = n_heads; g.units_per_layer = upl;
     g.cur_len = cur_len; g.n_sink = n_sink; g.n_recent = n_recent; g.keep = keep; g.cur_lens = cur_lens; g.capacity = L.token_capacity;
-    g.by_layer = divisor(upl); g.by_kv = divisor(n_heads); g.by_slice = divisor(g.slices); g.by_pieces = divisor(g.slice_pieces);
+    g.by_layer = divisor(upl); g.by_kv = divisor(n_heads); g.by_pieces = divisor(g.slice_pieces);
     g.stride_batch = L.stride_batch * elem; g.stride_head = L.stride_head * elem; g.stride_token = L.stride_token * elem;
     const bool due = cur_lens || (long long)cur_len - n_sink - n_recent > keep;
     for (int l0 = 0; l0 < L.n_layers; l0 += kLayersPerPass) {

@@ -351,7 +351,7 @@ __global__ __launch_bounds__(256) void k_weights_join(const WeightGeom g, const 
 
 namespace {
 
-constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64, kBins = 2048;
+constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
 
 // Larger weights have larger orders; +0 and -0 the same one, NaN the least.
 __device__ __forceinline__ uint32_t order_of(float w)
@@ -359,6 +359,28 @@ __device__ __forceinline__ uint32_t order_of(float w)
     const uint32_t u = __float_as_uint(w + 0.f);
     if ((u & 0x7fffffffu) > 0x7f800000u) return 0;
     return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+// Sum over the 16 lanes of a row, common to the wave where all rows have the same.  (Sixteen counts read by every lane, 16 waves of them, are what LDS would be busy with.)
+__device__ __forceinline__ int sum16(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x140, 0xf, 0xf, true);
+    return __builtin_amdgcn_readfirstlane(x);
+}
+
+// Sum over the wave, in its last lane.
+__device__ __forceinline__ int sum_wave(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);       // lanes 1, 2, 4 and 8 below, in rows of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // the last lane of a row to the next
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // ... of the second row to the third and fourth
+    return x;
 }
 
 // Rows of a sequence and of what competes in it.
@@ -375,14 +397,20 @@ __device__ __forceinline__ Span span_of(const EvictGeom& g, int b)
 
 }  // namespace
 
-// A workgroup to a unit.  The keep-th largest order is found 11, 11 and 10 bits at a time, from counts of the rows that agree in the bits before; of the rows
-// that have it the first ones stay.  Then rows are gone through in their order, 1024 at a time, and each of those that stay has its place from the
-// counts of those before it.  weights_out may be weights: rows are read ahead of a barrier, and move to lower places only.
-__global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictGeom g, const float* weights, float* weights_out, int* __restrict__ kept, int* __restrict__ new_lens)
+// A workgroup to a unit, a thread with R rows of its own, 1024 apart, in registers (R 0: more rows than that, read again each time).  The keep-th largest order is
+// found bit by bit, from counts of the rows at or above a candidate, until just the rows that stay are (with counters in LDS, rows of much the same weight queue
+// for the same one: 8192 rows 22 us, so 13.8, or 17.5 where equal weights take all 32 bits; two bits at a time 28); of the rows that have it the first ones stay.  Then every row that stays has its place from the counts of those before
+// it, by 64s, which a scan gives.  weights_out may be weights: all rows are read ahead of a barrier.
+template <int R>
+__global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictGeom, const float* weights, float* weights_out, int* __restrict__ kept, int* __restrict__ new_lens)
 {
-    __shared__ uint32_t hist[kBins];
-    __shared__ int above[kSelectWaves], chosen[2], counts[2][2][kSelectWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const EvictGeom g = first_argument<decltype(k_evict_select<R>)>();
+    constexpr int W = kSelectWaves, N = R ? R : 1;
+    static_assert(W == 16, "a count to each lane of 16");
+    __shared__ __attribute__((aligned(16))) int counts[2][2][W];
+    __shared__ int larger[N * W], equal[N * W];      // of each 64 rows, then of all rows before them
+    __shared__ int sums[2][W];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int unit = blockIdx.x, layer = g.by_layer.quotient(unit), rem = unit - layer * g.units_per_layer;
     const int b = g.by_kv.quotient(rem), kvh = rem - b * g.n_kv;
     const Span s = span_of(g, b);
@@ -400,103 +428,177 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictGeom
         }
         return;
     }
-    uint32_t found = 0;                              // bits of the keep-th largest order
-    int need = g.keep;                               // rows still to be taken among those that agree with them
-    for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-        for (int i = tid; i < kBins; i += kSelectThreads) hist[i] = 0;
-        __syncthreads();
-        for (int r = s.lo + tid; r < s.hi; r += kSelectThreads) {
-            const uint32_t u = order_of(w[r]);
-            if (pass == 0 || u >> (shift + bits) == found >> (shift + bits)) atomicAdd(&hist[u >> shift & ((1u << bits) - 1)], 1u);
+    const int rows = s.hi - s.lo, tiles = (rows + kSelectThreads - 1) / kSelectThreads;
+    float x[N];
+    uint32_t u[N];
+    static_for<R>([&](auto i) { const int r = i.value * kSelectThreads + tid; x[i.value] = r < rows ? w[s.lo + r] : 0.f; });
+    static_for<R>([&](auto i) { u[i.value] = order_of(x[i.value]); });
+    static_for<R>([&](auto i) { u[i.value] = i.value * kSelectThreads + tid < rows ? u[i.value] : 0u; });
+    // every row's order, tile by tile; rows past the end have the least, 0
+    auto each = [&](auto&& f) {
+        if constexpr (R > 0) {
+            static_for<R>([&](auto i) { f(i.value, i.value * kSelectThreads + tid < rows, u[i.value], x[i.value]); });
+        } else {
+            for (int i = 0; i < tiles; ++i) {
+                const int r = i * kSelectThreads + tid;
+                const float y = r < rows ? w[s.lo + r] : 0.f;
+                f(i, r < rows, r < rows ? order_of(y) : 0u, y);
+            }
         }
+    };
+    uint32_t found = 0;
+    for (int bit = 31, flip = 0; bit >= 0; --bit, flip ^= 1) {
+        const uint32_t candidate = found | 1u << bit;
+        int n = 0;
+        each([&](int, bool, uint32_t v, float) { n += v >= candidate; });
+        n = sum_wave(n);
+        if (lane == 63) counts[flip][0][wave] = n;
         __syncthreads();
-        // thread t has the bins 2047 - 2 t and 2046 - 2 t, from the largest down; the rows above them by a sum over the threads before
-        const int top = kBins - 1 - 2 * tid, c0 = (int)hist[top], c1 = (int)hist[top - 1];
-        int before = c0 + c1;
-        for (int o = 1; o < 64; o <<= 1) {
-            const int x = __shfl_up(before, o);
-            if (lane >= o) before += x;
+        n = sum16(counts[flip][0][lane & 15]);
+        if (n >= g.keep) found = candidate;
+        if (n == g.keep) {                           // just the rows that stay: all above the next lower order
+            --found;
+            break;
         }
-        if (lane == 63) above[wave] = before;
-        __syncthreads();
-        before -= c0 + c1;
-        for (int i = 0; i < wave; ++i) before += above[i];
-        if (before < need && before + c0 >= need) { chosen[0] = top; chosen[1] = before; }
-        else if (before + c0 < need && before + c0 + c1 >= need) { chosen[0] = top - 1; chosen[1] = before + c0; }
-        __syncthreads();
-        found |= (uint32_t)chosen[0] << shift;
-        need -= chosen[1];
-        __syncthreads();
     }
-    if (wo && wo != w)
-        for (int r = tid; r < s.lo; r += kSelectThreads) wo[r] = w[r];
-    int larger = 0, equal = 0;                       // among the rows so far
-    for (int r0 = s.lo, flip = 0; r0 < s.hi; r0 += kSelectThreads, flip ^= 1) {
-        const int r = r0 + tid;
-        const float x = r < s.hi ? w[r] : 0.f;
-        const uint32_t u = order_of(x);
-        const bool gt = r < s.hi && u > found, eq = r < s.hi && u == found;
-        const uint64_t mg = __builtin_amdgcn_ballot_w64(gt), me = __builtin_amdgcn_ballot_w64(eq);
-        if (lane == 0) { counts[flip][0][wave] = __popcll(mg); counts[flip][1][wave] = __popcll(me); }
-        __syncthreads();
-        int g0 = larger, e0 = equal;
-        for (int i = 0; i < kSelectWaves; ++i) {
-            if (i < wave) { g0 += counts[flip][0][i]; e0 += counts[flip][1][i]; }
-            larger += counts[flip][0][i];
-            equal += counts[flip][1][i];
+    // ---- rows above and at the order found, by 64s; `place` of the first row that stays of each
+    auto prefix = [&](int i, int& above, int& at) {  // counts of a tile's waves, and those before
+        above = larger[(R ? i : 0) * W + wave];
+        at = equal[(R ? i : 0) * W + wave];
+    };
+    int all_above = 0, all_at = 0;                   // R 0: of the tiles before
+    auto put = [&](int i, bool there, uint32_t v, float y, int need) {
+        const bool gt = there && v > found, eq = there && v == found;
+        const uint64_t mg = __builtin_amdgcn_ballot_w64(gt), me = __builtin_amdgcn_ballot_w64(eq), below = ((uint64_t)1 << lane) - 1;
+        int above, at;
+        prefix(i, above, at);
+        above += __popcll(mg & below);
+        at += __popcll(me & below);
+        if (gt || (eq && at < need)) {
+            const int place = above + min(at, need);
+            out[place] = s.lo + i * kSelectThreads + tid;
+            if (wo) wo[s.lo + place] = y;
         }
-        const uint64_t below = ((uint64_t)1 << lane) - 1;
-        g0 += __popcll(mg & below);
-        e0 += __popcll(me & below);
-        if (gt || (eq && e0 < need)) {
-            const int at = g0 + min(e0, need);
-            out[at] = r;
-            if (wo) wo[s.lo + at] = x;
+    };
+    if constexpr (R > 0) {
+        static_for<R>([&](auto i) {
+            const bool there = i.value * kSelectThreads + tid < rows;
+            const uint64_t mg = __builtin_amdgcn_ballot_w64(there && u[i.value] > found), me = __builtin_amdgcn_ballot_w64(there && u[i.value] == found);
+            if (lane == 0) { larger[i.value * W + wave] = __popcll(mg); equal[i.value * W + wave] = __popcll(me); }
+        });
+        __syncthreads();
+        // thread t < 16 R has the t-th 64 rows
+        const int a = tid < N * W ? larger[tid] : 0, e = tid < N * W ? equal[tid] : 0;
+        int ia = a, ie = e;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int ya = __shfl_up(ia, o), ye = __shfl_up(ie, o);
+            if (lane >= o) { ia += ya; ie += ye; }
+        }
+        if (lane == 63) { sums[0][wave] = ia; sums[1][wave] = ie; }
+        __syncthreads();
+        const int sa = sums[0][lane & 15], se = sums[1][lane & 15], total = sum16(sa);
+        const int ba = sum16((lane & 15) < wave ? sa : 0), be = sum16((lane & 15) < wave ? se : 0);
+        if (tid < N * W) { larger[tid] = ba + ia - a; equal[tid] = be + ie - e; }
+        __syncthreads();
+        each([&](int i, bool there, uint32_t v, float y) { put(i, there, v, y, g.keep - total); });
+    } else {
+        int total = 0;
+        each([&](int, bool there, uint32_t v, float) { total += __popcll(__builtin_amdgcn_ballot_w64(there && v > found)); });
+        if (lane == 0) sums[0][wave] = total;
+        __syncthreads();
+        total = sum16(sums[0][lane & 15]);
+        for (int i = 0, flip = 0; i < tiles; ++i, flip ^= 1) {
+            const int r = i * kSelectThreads + tid;
+            const float y = r < rows ? w[s.lo + r] : 0.f;
+            const uint32_t v = order_of(y);
+            const uint64_t mg = __builtin_amdgcn_ballot_w64(r < rows && v > found), me = __builtin_amdgcn_ballot_w64(r < rows && v == found);
+            if (lane == 0) { counts[flip][0][wave] = __popcll(mg); counts[flip][1][wave] = __popcll(me); }
+            __syncthreads();
+            const int ca = counts[flip][0][lane & 15], ce = counts[flip][1][lane & 15];
+            const int above = all_above + sum16((lane & 15) < wave ? ca : 0), at = all_at + sum16((lane & 15) < wave ? ce : 0);
+            all_above += sum16(ca);
+            all_at += sum16(ce);
+            if (lane == 0) { larger[wave] = above; equal[wave] = at; }
+            asm volatile("" ::: "memory");           // (a wave's own, in order)
+            put(i, r < rows, v, y, g.keep - total);
         }
     }
     if (!wo) return;
+    if (wo != w)
+        for (int r = tid; r < s.lo; r += kSelectThreads) wo[r] = w[r];
     for (int r0 = s.hi; r0 < s.n; r0 += kSelectThreads) {
         const int r = r0 + tid;
-        const float x = r < s.n ? w[r] : 0.f;
+        const float y = r < s.n ? w[r] : 0.f;
         __syncthreads();
-        if (r < s.n) wo[s.lo + g.keep + (r - s.hi)] = x;
+        if (r < s.n) wo[s.lo + g.keep + (r - s.hi)] = y;
     }
     __syncthreads();
     for (int r = new_len + tid; r < g.cur_len; r += kSelectThreads) wo[r] = 0.f;
 }
 
-// A workgroup moves a slice of all rows of a head-tensor, in their order: 64 KB are read, and after a barrier written, to lower rows.  No row is written that is
-// still to be read: the i-th row that stays lies at lo + i or above, and the rows written until then are those up to there.
+// A workgroup moves a slice of all rows of a head-tensor, in their order, 64 KB at a time: read, and after a barrier written, to lower rows.  No row is written that is
+// still to be read: the i-th row that stays lies at lo + i or above, and the rows written until then are those up to there; so the next 64 KB are asked for ahead of the
+// writes, and which rows they are another step ahead.  A barrier waits for the rows asked for before it alone.  Slices of a head-tensor's rows go to one XCD, whose L2 puts lines
+// together.
 constexpr int kMovePieces = 4;
+__device__ __forceinline__ void awaited(u32x4& x) { asm volatile("" : "+v"(x)); }
 __global__ __launch_bounds__(1024) void k_evict_move(const EvictGeom, const int* __restrict__ kept, const SlabTable tab)
 {
     const EvictGeom g = first_argument<decltype(k_evict_move)>();
-    const int us = g.by_slice.quotient(blockIdx.x), slice = blockIdx.x - us * g.slices, unit = us >> 1, kv = us & 1;
+    int us = blockIdx.x, slice = 0;
+    if (g.slices > 1) share_out(g.slices, us, slice);
+    const int unit = us >> 1, kv = us & 1;
     const int layer = g.by_layer.quotient(unit), rem = unit - layer * g.units_per_layer;
     const int b = g.by_kv.quotient(rem), kvh = rem - b * g.n_kv;
     const Span s = span_of(g, b);
     if (!s.due) return;
     char* const base = tab.base[2 * layer + kv] + (long long)b * g.stride_batch + (long long)kvh * g.stride_head + (long long)slice * g.slice_pieces * 16;
     const int* const from = kept + (long long)unit * g.keep;
-    const int rows = g.keep + (s.n - s.hi);
-    const int per_step = 1024 * kMovePieces;
-    const long long pieces = (long long)rows * g.slice_pieces;
-    for (long long p0 = 0; p0 < pieces; p0 += per_step) {
-        u32x4 x[kMovePieces];
-        char* to[kMovePieces];
+    constexpr int STEP = 1024 * kMovePieces;
+    const int pieces = (g.keep + (s.n - s.hi)) * g.slice_pieces, steps = (pieces + STEP - 1) / STEP;
+    // the i-th piece of a step that a thread has: row it comes from (past the end: the last one's again, not written)
+    struct Step { u32x4 x[kMovePieces]; };
+    int src[kMovePieces];
+    auto which = [&](int t) {
         static_for<kMovePieces>([&](auto i) {
-            const long long p = p0 + i.value * 1024 + (int)threadIdx.x;
-            to[i.value] = nullptr;
-            if (p < pieces) {
-                const int row = g.by_pieces.quotient((int)p), piece = (int)p - row * g.slice_pieces;
-                const int src = row < g.keep ? from[row] : s.hi + (row - g.keep);
-                x[i.value] = *(const u32x4*)(base + (long long)src * g.stride_token + piece * 16);
-                to[i.value] = base + (long long)(s.lo + row) * g.stride_token + piece * 16;
-            }
+            const int row = g.by_pieces.quotient(min(t * STEP + i.value * 1024 + (int)threadIdx.x, pieces - 1));
+            src[i.value] = row < g.keep ? from[row] : s.hi + (row - g.keep);
         });
-        __syncthreads();
-        static_for<kMovePieces>([&](auto i) { if (to[i.value]) *(u32x4*)to[i.value] = x[i.value]; });
+    };
+    auto ask = [&](Step& x, int t) {
+        static_for<kMovePieces>([&](auto i) {
+            const int p = min(t * STEP + i.value * 1024 + (int)threadIdx.x, pieces - 1), row = g.by_pieces.quotient(p);
+            x.x[i.value] = *(const u32x4*)(base + (long long)src[i.value] * g.stride_token + (p - row * g.slice_pieces) * 16);
+        });
+    };
+    auto put = [&](const Step& x, int t) {
+        static_for<kMovePieces>([&](auto i) {
+            const int p = t * STEP + i.value * 1024 + (int)threadIdx.x, row = g.by_pieces.quotient(p);
+            if (p < pieces) *(u32x4*)(base + (long long)(s.lo + row) * g.stride_token + (p - row * g.slice_pieces) * 16) = x.x[i.value];
+        });
+    };
+    auto arrived = [&](Step& x) {                    // ... in all threads of the workgroup
+        static_for<kMovePieces>([&](auto i) { awaited(x.x[i.value]); });
+        asm volatile("s_barrier" ::: "memory");
+    };
+    Step a, c;
+    which(0);
+    ask(a, 0);
+    if (steps > 1) which(1);
+    for (int t = 0; t < steps; t += 2) {
+        arrived(a);
+        if (t + 1 < steps) {
+            ask(c, t + 1);
+            if (t + 2 < steps) which(t + 2);
+        }
+        put(a, t);
+        if (t + 1 >= steps) break;
+        arrived(c);
+        if (t + 2 < steps) {
+            ask(a, t + 2);
+            if (t + 3 < steps) which(t + 3);
+        }
+        put(c, t + 1);
     }
 }
 
@@ -553,8 +655,12 @@ hipError_t launch_weights(const SlabTable& tab, const WeightGeom& g, const void*
 
 hipError_t launch_evict_select(const EvictGeom& g, const float* weights, float* weights_out, int* kept, int* new_lens, hipStream_t st)
 {
-    hipLaunchKernelGGL(k_evict_select, dim3((unsigned)g.units), dim3(kSelectThreads), 0, st, g, weights, weights_out, kept, new_lens);
-    return hipGetLastError();
+    const int tiles = (g.cur_len + kSelectThreads - 1) / kSelectThreads;       // (rows that compete: at most)
+    auto launch = [&](auto r) {
+        hipLaunchKernelGGL(k_evict_select<decltype(r)::value>, dim3((unsigned)g.units), dim3(kSelectThreads), 0, st, g, weights, weights_out, kept, new_lens);
+        return hipGetLastError();
+    };
+    return tiles <= 2 ? launch(IC<2>{}) : tiles <= 8 ? launch(IC<8>{}) : tiles <= 32 ? launch(IC<32>{}) : launch(IC<0>{});
 }
 
 hipError_t launch_evict_move(const SlabTable& tab, const EvictGeom& g, const int* kept, hipStream_t st)

@@ -430,7 +430,7 @@ struct EvictGeom {
     int cur_len, n_sink, n_recent, keep;
     const int* cur_lens;               // optional device array [batch]
     int capacity;                      // rows of `weights`
-    Divisor by_layer, by_kv, by_slice, by_pieces;
+    Divisor by_layer, by_kv, by_pieces;
     long long stride_batch, stride_head, stride_token;   // bytes
 };
 // new_lens: of the whole batch, written by the first layer's units (first_layer)

@@ -260,3 +260,17 @@ def test_replayed_graph_of_the_two():
             state.append([x.clone() for x in (k, v, w, kept, new)])
         assert all(torch.equal(a, b) for a, b in zip(*state))
     del ws
+
+
+@pytest.mark.parametrize("T,keep", [(2049, 700), (9000, 4500), (33000, 9), (40000, 20000)])
+def test_evict_long(T, keep):
+    """Rows of a thread in registers, two, eight or 32 of them, and more rows than that."""
+    print(T, keep, flush=True)
+    k, v, w = _case(1, 1, 2, T, 16, torch.bfloat16, 17)
+    w[0, 0, 1] = 0.5
+    w[0, 0, 1, ::7] = 1.5
+    k0, v0, w0 = k.clone(), v.clone(), w.clone()
+    for wo in ("new", "same"):
+        k, v, w = k0.clone(), v0.clone(), w0.clone()
+        w_out, kept, new = _evict(k, v, w, T, 4, 100, keep, wo=wo)
+        _verify(k0, v0, w0, k, v, w_out, kept, new, T, None, 4, 100, keep)
