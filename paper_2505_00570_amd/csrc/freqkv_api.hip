@@ -1917,7 +1917,7 @@ freqkv_status_t check_weights(const freqkv_layout_t* L, int n_q, int n_kv, int d
         if (w.units * w.n_chunk >= 1 << 23) return FREQKV_E_UNSUPPORTED;
     } else {
         w.q_tiles = (w.M + kWeightTile - 1) / kWeightTile;
-        w.key_blocks = (cur_len + kWeightKeys - 1) / kWeightKeys;
+        w.key_blocks = (cur_len + weight_keys(d) - 1) / weight_keys(d);
         const long long wgs = w.units * w.key_blocks;
         const long long ns = std::min((long long)w.q_tiles, std::max(1LL, 1024 / wgs));
         w.split_tiles = (int)((w.q_tiles + ns - 1) / ns);
@@ -2051,7 +2051,7 @@ freqkv_status_t freqkv_attend_weights_plan(const freqkv_layout_t* layout, int n_
     if (rc < 0) return rc;
     memset(out, 0, sizeof(*out));
     out->n_split = w.M <= kWeightFew ? w.n_chunk : w.n_split;
-    out->chunk_rows = w.M <= kWeightFew ? w.chunk : kWeightKeys;
+    out->chunk_rows = w.M <= kWeightFew ? w.chunk : weight_keys(head_dim);
     out->heads_together = std::min(w.M, w.M <= kWeightFew ? kWeightFew : kWeightTile);
     out->workspace_bytes = w.workspace_bytes;
     const double seen = (double)q_len * (cur_len - q_len) + 0.5 * (double)q_len * (q_len + 1);

@@ -2,8 +2,8 @@
 //
 // The weight of row p of a KV head is the sum, over queries i and the heads that share the KV head, of exp(s_ip - lse_i): the softmax weights that attention
 // has given the row.  The results are fp32 sums of many positive terms, and an error of the scores is a relative one of the weights, so scores are made to
-// 22 bits: each turned key and query is a sum of two fp16 numbers, and three of the four products of those are taken, on the matrix cores in fp32.
-// Keys and queries are divided by powers of two of their own (largest element of a row 2^12 .. 2^13), which come back in fp32: fp16 holds any magnitude.
+// 22 bits or more: in fp32 where there are few queries, else each turned key and query is a sum of two fp16 numbers, and three of the four products of those are taken.
+// Queries, and tiles of keys, are then divided by powers of two (largest element 2^12 .. 2^13), which come back in fp32: fp16 holds any magnitude.
 //
 //   k_weights_few      up to 16 queries of a unit: rows stream by, queries stay
 //   k_weights_queries  more: the queries as operands, turned, in fragment order
@@ -58,21 +58,24 @@ __device__ __forceinline__ void split8(const float (&x)[8], half8& hi, half8& lo
     });
 }
 
+__device__ __forceinline__ void pin(half8& x) { asm volatile("" : "+v"(x) :: "memory"); }
+
 // log2(e) times a query's lse, to be taken from its scores.  One that saw no row (-inf) adds nothing.
 __device__ __forceinline__ float taken(float lse) { return lse == -INFINITY ? INFINITY : lse * 1.4426950408889634f; }
 
 }  // namespace
 
 // Up to 16 queries: bound by the rows.  A wave has tiles of 16 rows; a lane (c, g) = (lane & 15, lane >> 4) has of row c the channels 32 p + 8 g .. + 7 for every p,
-// so that a rotary pair is in one lane, and gets the scores of row c with the queries 4 g .. 4 g + 3.
+// so that a rotary pair is in one lane, and gets the scores of row c with the queries 4 g .. 4 g + 3.  v_mfma_f32_16x16x4_f32: products and sums in fp32, nothing to split (with
+// keys and queries as sums of two fp16 a tile took 390 vector instructions instead of 190: 16 sequences of 4096 to 8192 rows, 8 KV heads, 76 us).
 template <typename T, int D>
-__global__ __launch_bounds__(256, (D == 256 ? 1 : 2))
+__global__ __launch_bounds__(256, (D == 256 ? 1 : sizeof(T) == 4 ? 2 : 3))
 void k_weights_few(const WeightGeom, const T* __restrict__ q, const float* __restrict__ lse, const TurnTable rt, float* __restrict__ weights,
                    const SlabTable tab)
 {
     const WeightGeom g = first_argument<decltype(k_weights_few<T, D>)>();
-    constexpr int KS = D / 32, HP = KS / 2;         // k-steps; of a half
-    __shared__ __attribute__((aligned(16))) float2 turns[4][D / 2];
+    constexpr int HP = D / 64;                      // pieces of eight channels of a lane in each half
+    __shared__ __attribute__((aligned(16))) float2 turns[4][D];       // of each wave: where seeds come from, and the rotations by a step
     const int lane = threadIdx.x & 63, c = lane & 15, gq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int unit = g.by_chunk.quotient(blockIdx.x), ck = blockIdx.x - unit * g.n_chunk;
@@ -89,103 +92,84 @@ void k_weights_few(const WeightGeom, const T* __restrict__ q, const float* __res
 
     const int wrow = row0 + 16 * wave, tiles = wrow < row_end ? (row_end - wrow + kTurnStep - 1) / kTurnStep : 0;
     Eight<T> lo[HP], up[HP];
+    float old = 0.f;                                 // of the weight that the lane writes
     auto load = [&](int n) {
-        const uint32_t at = (uint32_t)(wrow + n * kTurnStep + c) * row_bytes + (uint32_t)(8 * gq) * (uint32_t)sizeof(T);
+        const int row = wrow + n * kTurnStep + c;
+        const uint32_t at = (uint32_t)row * row_bytes + (uint32_t)(8 * gq) * (uint32_t)sizeof(T);
         static_for<HP>([&](auto p) {
             read8(kbuf, at + p.value * 32 * (uint32_t)sizeof(T), lo[p.value]);
             read8(kbuf, at + (D / 2 + p.value * 32) * (uint32_t)sizeof(T), up[p.value]);
         });
+        if (g.accumulate) old = wout[min(row, row_end - 1)];
     };
     load(0);
-    float co[HP][8], si[HP][8], cd[HP][8], sd[HP][8];
+    float co[HP][8], si[HP][8];
     float2* const own = turns[wave];
     auto seed = [&](int n) {
         wave_turns<D>(rt, wrow + n * kTurnStep - (cur_len - 1), own, lane);
         static_for<HP>([&](auto p) { seeds<D, 8>(rt, own, c, 32 * p.value + 8 * gq, co[p.value], si[p.value]); });
     };
-    static_for<HP>([&](auto p) { steps<8>(rt, 32 * p.value + 8 * gq, cd[p.value], sd[p.value]); });
+    static_for<(D / 2 + 63) / 64>([&](auto n) { if (n.value * 64 + lane < D / 2) own[D / 2 + n.value * 64 + lane] = rt.step[n.value * 64 + lane]; });
     seed(0);
 
-    // ---- queries: the lane's is c; of those that its scores are of, factors, lse and last rows
-    half8 qh[KS], ql[KS];
+    // ---- queries: the lane's is c, scaled by log2(e) / sqrt(d), turned by its place less the last one's; of those that its scores are of, lse and last rows
+    float ql[HP][8], qu[HP][8];
     const long long head0 = (long long)unit * g.M;
     const int mine = min(c, g.M - 1), place = mine - g.by_q.quotient(mine) * g.q_len;
-    float qfactor;
     {
-        Eight<T> a[HP], bb[HP];
         const T* const qp = q + (head0 + mine) * D + 8 * gq;
-        float most = 0.f;
         static_for<HP>([&](auto p) {
-            read8(qp + 32 * p.value, a[p.value]);
-            read8(qp + D / 2 + 32 * p.value, bb[p.value]);
-            static_for<8>([&](auto i) { most = fmaxf(most, fmaxf(fabsf(at8<i.value>(a[p.value])), fabsf(at8<i.value>(bb[p.value])))); });
-        });
-        most = fold<32>(fold<16>(most, Max{}), Max{});
-        const Power pw = power_for(most);
-        qfactor = pw.up * g.qscale;
-        static_for<HP>([&](auto p) {
-            float x[8], y[8];
-            static_for<8>([&](auto i) { x[i.value] = at8<i.value>(a[p.value]) * pw.down; y[i.value] = at8<i.value>(bb[p.value]) * pw.down; });
+            Eight<T> a, bb;
+            read8(qp + 32 * p.value, a);
+            read8(qp + D / 2 + 32 * p.value, bb);
+            static_for<8>([&](auto i) { ql[p.value][i.value] = at8<i.value>(a) * g.qscale; qu[p.value][i.value] = at8<i.value>(bb) * g.qscale; });
             if (g.q_len > 1) {
                 static_for<8>([&](auto i) {
-                    const float l = x[i.value], u = y[i.value];
+                    const float l = ql[p.value][i.value], u = qu[p.value][i.value];
                     const CosSin t = turn(rt.quarters[32 * p.value + 8 * gq + i.value], place + 1 - g.q_len);
-                    x[i.value] = fmaf(l, t.c, -(u * t.s));
-                    y[i.value] = fmaf(u, t.c, l * t.s);
+                    ql[p.value][i.value] = fmaf(l, t.c, -(u * t.s));
+                    qu[p.value][i.value] = fmaf(u, t.c, l * t.s);
                     if constexpr (i.value % 4 == 3) __builtin_amdgcn_sched_barrier(0);    // (all at once, they take more registers than there are)
                 });
             }
-            split8(x, qh[p.value], ql[p.value]);
-            split8(y, qh[HP + p.value], ql[HP + p.value]);
         });
     }
     const float taken_mine = c < g.M ? taken(lse[head0 + mine]) : INFINITY;      // (no query there: nothing is added)
-    float factor[4], minus[4];
+    float less[4];
     int last[4];                                     // row of the query
     static_for<4>([&](auto r) {
-        factor[r.value] = __shfl(qfactor, 4 * gq + r.value);
-        minus[r.value] = -__shfl(taken_mine, 4 * gq + r.value);
+        less[r.value] = __shfl(taken_mine, 4 * gq + r.value);
         last[r.value] = cur_len - g.q_len + __shfl(place, 4 * gq + r.value);
     });
 
     for (int n = 0; n < tiles; ++n) {
         if (n > 0 && n % 64 == 0) seed(n);
-        half8 kh[KS], kl[KS];
-        float most = 0.f;
+        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+        int ln = lane;
+        asm volatile("" : "+v"(ln));                 // (rotations are read in every step, and not kept in registers from before the loop)
         static_for<HP>([&](auto p) {
-            static_for<8>([&](auto i) { most = fmaxf(most, fmaxf(fabsf(at8<i.value>(lo[p.value])), fabsf(at8<i.value>(up[p.value])))); });
-        });
-        most = fold<32>(fold<16>(most, Max{}), Max{});
-        const Power pw = power_for(most);
-        static_for<HP>([&](auto p) {
-            float x[8], y[8];
             static_for<8>([&](auto i) {
                 constexpr int P = p.value, I = i.value;
-                const float l = at8<I>(lo[P]) * pw.down, u = at8<I>(up[P]) * pw.down;
-                x[I] = fmaf(l, co[P][I], -(u * si[P][I]));
-                y[I] = fmaf(u, co[P][I], l * si[P][I]);
-                const float cn = fmaf(co[P][I], cd[P][I], -(si[P][I] * sd[P][I]));
-                si[P][I] = fmaf(si[P][I], cd[P][I], co[P][I] * sd[P][I]);
+                const float l = at8<I>(lo[P]), u = at8<I>(up[P]);
+                const float x = fmaf(l, co[P][I], -(u * si[P][I])), y = fmaf(u, co[P][I], l * si[P][I]);
+                const float2 by = own[D / 2 + 32 * P + 8 * (ln >> 4) + I];
+                const float cn = fmaf(co[P][I], by.x, -(si[P][I] * by.y));
+                si[P][I] = fmaf(si[P][I], by.x, co[P][I] * by.y);
                 co[P][I] = cn;
+                s = __builtin_amdgcn_mfma_f32_16x16x4f32(ql[P][I], x, s, 0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_16x16x4f32(qu[P][I], y, s, 0, 0, 0);
             });
-            split8(x, kh[p.value], kl[p.value]);
-            split8(y, kh[HP + p.value], kl[HP + p.value]);
         });
+        const float before = old;
         if (n + 1 < tiles) load(n + 1);
-        f32x4 s = {0.f, 0.f, 0.f, 0.f};
-        static_for<KS>([&](auto k) {
-            s = __builtin_amdgcn_mfma_f32_16x16x32_f16(ql[k.value], kh[k.value], s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_16x16x32_f16(qh[k.value], kl[k.value], s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_16x16x32_f16(qh[k.value], kh[k.value], s, 0, 0, 0);
-        });
         const int row = wrow + n * kTurnStep + c;
         float w = 0.f;
         static_for<4>([&](auto r) {
-            const float e = exp2_fast(fmaf(s[r.value], factor[r.value] * pw.up, minus[r.value]));
+            const float e = exp2_fast(s[r.value] - less[r.value]);
             w += row <= last[r.value] ? e : 0.f;
         });
         w = fold<32>(fold<16>(w, Add{}), Add{});
-        if (gq == 0 && row < row_end) wout[row] = g.accumulate ? wout[row] + w : w;
+        if (gq == 0 && row < row_end) wout[row] = before + w;
     }
 }
 
@@ -234,15 +218,16 @@ __global__ __launch_bounds__(256) void k_weights_queries(const WeightGeom, const
     if (sub == 0) factors[((long long)unit * g.q_tiles + tile) * kWeightTile + j] = float2{there ? pw.up * g.qscale : 0.f, there ? -taken(lse[head]) : -INFINITY};
 }
 
-// More queries: bound by the matrix cores.  A wave has 32 keys, a workgroup 128; v_mfma_f32_32x32x16_f16, queries x keys, so that a lane gets 16 queries' scores with one
-// key, and adds up weights without an exchange.
+// More queries: bound by the matrix cores.  A wave has KT tiles of 32 keys, in registers; v_mfma_f32_32x32x16_f16, keys x queries, so that a lane has one query's
+// scores with 16 keys of a tile: its lse and factor are one number each, and weights add up, over all queries, without an exchange until the end.  A tile of queries, 16 KB
+// at d = 128, comes from the L2 once for each wave; two tiles of keys use it twice (one: 2.0 TB/s asked of the first-level cache, which is what it gives).
 template <typename T, int D>
 __global__ __launch_bounds__(256, (D == 256 ? 1 : 2))
 void k_weights(const WeightGeom, const _Float16* __restrict__ operands, const float2* __restrict__ factors, const TurnTable rt,
                float* __restrict__ parts, float* __restrict__ weights, const SlabTable tab)
 {
     const WeightGeom g = first_argument<decltype(k_weights<T, D>)>();
-    constexpr int KS = D / 16, HP = KS / 2;         // k-steps; of a half
+    constexpr int KS = D / 16, HP = KS / 2, KT = weight_key_tiles(D), KEYS = kWeightTile * KT;         // k-steps; of a half; keys of a wave
     static_assert(kWeightTile <= kTurnRows, "rows of a tile");
     __shared__ __attribute__((aligned(16))) float2 turns[4][D / 2];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hw = lane >> 5;
@@ -254,30 +239,35 @@ void k_weights(const WeightGeom, const _Float16* __restrict__ operands, const fl
     const int b = g.by_kv.quotient(rem), kvh = rem - b * g.n_kv;
     int cur_len = g.cur_len;
     if (g.cur_lens) cur_len = max(0, min(g.cur_lens[b], g.cur_len));
-    const int row0 = kb * kWeightKeys + wave * kWeightTile, row = row0 + l32;
+    const int row0 = (kb * 4 + wave) * KEYS;
     if (row0 >= cur_len) return;
     const uint32_t row_bytes = (uint32_t)g.stride_token * (uint32_t)sizeof(T);
     const char* const kbase = tab.base[layer] + ((long long)b * g.stride_batch + (long long)kvh * g.stride_head) * (long long)sizeof(T);
     const __amdgpu_buffer_rsrc_t kbuf = __builtin_amdgcn_make_buffer_rsrc((void*)kbase, 0, (int)((uint32_t)(cur_len - 1) * row_bytes + (uint32_t)(D * sizeof(T))), kBufferFlags);
 
-    half8 kh[KS], kl[KS];
-    float kfactor;
-    {
+    // ---- keys, turned by their position less the last row's, divided by a power of two common to a tile
+    half8 kh[KT][KS], kl[KT][KS];
+    float kfactor[KT];
+    float2* const own = turns[wave];
+    static_for<KT>([&](auto kt) {
+        const int first = row0 + kt.value * kWeightTile;
         Eight<T> lo[HP], up[HP];
-        const uint32_t at = (uint32_t)row * row_bytes + (uint32_t)(8 * hw) * (uint32_t)sizeof(T);
+        const uint32_t at = (uint32_t)(first + l32) * row_bytes + (uint32_t)(8 * hw) * (uint32_t)sizeof(T);
         float most = 0.f;
         static_for<HP>([&](auto p) {
             read8(kbuf, at + p.value * 16 * (uint32_t)sizeof(T), lo[p.value]);
             read8(kbuf, at + (D / 2 + p.value * 16) * (uint32_t)sizeof(T), up[p.value]);
         });
+        wave_turns<D>(rt, first - (cur_len - 1), own, lane);
         static_for<HP>([&](auto p) {
-            static_for<8>([&](auto i) { most = fmaxf(most, fmaxf(fabsf(at8<i.value>(lo[p.value])), fabsf(at8<i.value>(up[p.value])))); });
+            static_for<8>([&](auto i) {
+                // (of finite values: a row that is not keeps to itself)
+                const float a = fabsf(at8<i.value>(lo[p.value])), c = fabsf(at8<i.value>(up[p.value]));
+                most = fmaxf(most, fmaxf(a < INFINITY ? a : 0.f, c < INFINITY ? c : 0.f));
+            });
         });
-        most = fold<32>(most, Max{});
-        const Power pw = power_for(most);
-        kfactor = pw.up;
-        float2* const own = turns[wave];
-        wave_turns<D>(rt, row0 - (cur_len - 1), own, lane);
+        const Power pw = power_for(wave_fold(most, Max{}));
+        kfactor[kt.value] = pw.up;
         static_for<HP>([&](auto p) {
             float x[8], y[8], tc[8], ts[8];
             seeds<D, 8>(rt, own, l32, 16 * p.value + 8 * hw, tc, ts);
@@ -286,50 +276,73 @@ void k_weights(const WeightGeom, const _Float16* __restrict__ operands, const fl
                 x[i.value] = fmaf(l, tc[i.value], -(u * ts[i.value]));
                 y[i.value] = fmaf(u, tc[i.value], l * ts[i.value]);
             });
-            split8(x, kh[p.value], kl[p.value]);
-            split8(y, kh[HP + p.value], kl[HP + p.value]);
+            split8(x, kh[kt.value][p.value], kl[kt.value][p.value]);
+            split8(y, kh[kt.value][HP + p.value], kl[kt.value][HP + p.value]);
+            // (worked out here, one after the other: all at once they take more registers than there are)
+            pin(kh[kt.value][p.value]); pin(kl[kt.value][p.value]); pin(kh[kt.value][HP + p.value]); pin(kl[kt.value][HP + p.value]);
+            __builtin_amdgcn_sched_barrier(0);
         });
-    }
+    });
 
-    const int t0 = split * g.split_tiles, t1 = min(t0 + g.split_tiles, g.q_tiles);
-    float sum = 0.f;
+    const int t0 = split * g.split_tiles, t1 = min(t0 + g.split_tiles, g.q_tiles), past = cur_len - g.q_len;      // past: row of the query at place 0
+    // which tiles of queries see a key of the wave: places go from place0 on, and from 0 again where a head's chunk ends
+    f32x16 sum[KT];
+    static_for<KT>([&](auto kt) { static_for<16>([&](auto r) { sum[kt.value][r.value] = 0.f; }); });
+    constexpr int AHEAD = 2;                         // k-steps that a tile's queries are asked for ahead of their use
+    const half8* const ops = (const half8*)(operands + (long long)unit * g.q_tiles * (2 * kWeightTile * D)) + lane;
+    half8 qh[AHEAD], ql[AHEAD];
+    auto ask = [&](int t, auto k) {
+        const half8* const op = ops + (long long)t * (2 * KS * 64);
+        qh[k.value % AHEAD] = op[k.value * 64];
+        ql[k.value % AHEAD] = op[(KS + k.value) * 64];
+    };
     for (int t = t0; t < t1; ++t) {
-        // places of the tile's queries: from place0 on, and from 0 again where a head's chunk ends
         const int j0 = t * kWeightTile, n = min(kWeightTile, g.M - j0), place0 = j0 - g.by_q.quotient(j0) * g.q_len;
         const bool wraps = place0 + n > g.q_len;
-        const int past = cur_len - g.q_len;          // row of the query at place 0
-        if (row0 > past + (wraps ? g.q_len - 1 : place0 + n - 1)) continue;      // no query of the tile sees a key of the wave
-        const bool masked = row0 + kWeightTile - 1 > past + (wraps ? 0 : place0);
-        const half8* const op = (const half8*)(operands + ((long long)unit * g.q_tiles + t) * (2 * kWeightTile * D)) + lane;
-        f32x16 s;
-        static_for<16>([&](auto r) { s[r.value] = 0.f; });
+        if (row0 > past + (wraps ? g.q_len - 1 : place0 + n - 1)) continue;
+        static_for<AHEAD>([&](auto k) { ask(t, k); });
+        const float2 of_query = factors[((long long)unit * g.q_tiles + t) * kWeightTile + l32];
+        f32x16 s[KT];
+        static_for<KT>([&](auto kt) { static_for<16>([&](auto r) { s[kt.value][r.value] = 0.f; }); });
         static_for<KS>([&](auto k) {
-            const half8 h = op[k.value * 64], l = op[(KS + k.value) * 64];
-            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(l, kh[k.value], s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(h, kl[k.value], s, 0, 0, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x16_f16(h, kh[k.value], s, 0, 0, 0);
+            const half8 h = qh[k.value % AHEAD], l = ql[k.value % AHEAD];
+            static_for<KT>([&](auto kt) { s[kt.value] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kl[kt.value][k.value], h, s[kt.value], 0, 0, 0); });
+            static_for<KT>([&](auto kt) { s[kt.value] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh[kt.value][k.value], l, s[kt.value], 0, 0, 0); });
+            static_for<KT>([&](auto kt) { s[kt.value] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh[kt.value][k.value], h, s[kt.value], 0, 0, 0); });
+            if constexpr (k.value + AHEAD < KS) ask(t, IC<k.value + AHEAD>{});
         });
-        const float2* const fa = factors + ((long long)unit * g.q_tiles + t) * kWeightTile;
+        const bool masked = row0 + KEYS - 1 > past + (wraps ? 0 : place0);
+        const int at = j0 + l32, last = past + at - g.by_q.quotient(at) * g.q_len;       // row of the lane's query (one that there is not adds nothing)
+        static_for<KT>([&](auto kt) {
+            const float f = kfactor[kt.value] * of_query.x;
+            static_for<16>([&](auto r) {
+                float e = exp2_fast(fmaf(s[kt.value][r.value], f, of_query.y));
+                if (masked) e = row0 + kt.value * kWeightTile + 8 * (r.value / 4) + 4 * hw + r.value % 4 <= last ? e : 0.f;
+                sum[kt.value][r.value] += e;
+            });
+        });
+    }
+    // ---- over the queries of a tile; then lane r of 16 has the key of the register r
+    static_for<KT>([&](auto kt) {
+        float mine = 0.f;
         static_for<16>([&](auto r) {
-            const int j = 8 * (r.value / 4) + 4 * hw + r.value % 4;
-            const float2 f = fa[j];
-            float e = exp2_fast(fmaf(s[r.value], kfactor * f.x, f.y));
-            if (masked) {
-                const int at = j0 + j, place = at - g.by_q.quotient(at) * g.q_len;
-                e = row <= past + place && at < g.M ? e : 0.f;
-            }
-            sum += e;
+            float x = sum[kt.value][r.value];
+            x += dpp<0xB1>(x);
+            x += dpp<0x4E>(x);
+            x += dpp<0x141>(x);
+            x = fold<16>(fold<8>(x, Add{}), Add{});
+            mine = (lane & 15) == r.value ? x : mine;
         });
-    }
-    sum = fold<32>(sum, Add{});
-    if (hw == 0 && row < cur_len) {
-        if (g.n_split > 1) {
-            parts[((long long)split * g.units + unit) * g.cur_len + row] = sum;
-        } else {
-            float* const w = weights + (long long)unit * g.capacity + row;
-            *w = g.accumulate ? *w + sum : sum;
+        const int r = lane & 15, row = row0 + kt.value * kWeightTile + 8 * (r / 4) + 4 * hw + r % 4;
+        if ((lane & 16) == 0 && row < cur_len) {
+            if (g.n_split > 1) {
+                parts[((long long)split * g.units + unit) * g.cur_len + row] = mine;
+            } else {
+                float* const w = weights + (long long)unit * g.capacity + row;
+                *w = g.accumulate ? *w + mine : mine;
+            }
         }
-    }
+    });
 }
 
 __global__ __launch_bounds__(256) void k_weights_join(const WeightGeom g, const float* __restrict__ parts, float* __restrict__ weights)
@@ -641,7 +654,7 @@ hipError_t launch_weights_queries(const WeightGeom& g, const void* q, const floa
 hipError_t launch_weights(const SlabTable& tab, const WeightGeom& g, const void* operands, const float2* factors, const TurnTable& rt, float* parts,
                           float* weights, hipStream_t st)
 {
-    if (g.key_blocks != (g.cur_len + kWeightKeys - 1) / kWeightKeys || (long long)g.n_split * g.split_tiles < g.q_tiles) return hipErrorInvalidValue;
+    if (g.key_blocks != (g.cur_len + weight_keys(g.d) - 1) / weight_keys(g.d) || (long long)g.n_split * g.split_tiles < g.q_tiles) return hipErrorInvalidValue;
     hipError_t e = by_type(g, [&](auto t, auto d) {
         typedef decltype(t) T;
         hipLaunchKernelGGL((k_weights<T, decltype(d)::value>), dim3((unsigned)(g.units * g.n_split * g.key_blocks)), dim3(256), 0, st, g,

@@ -399,8 +399,9 @@ hipError_t launch_attend_q8(const SlabTable& tab, const Q8AttGeom& g, const void
 
 // ---- attention weights of the cached rows, and eviction by them -----------------------------------------
 constexpr int kWeightFew = 16;         // queries of a unit that k_weights_few takes
-constexpr int kWeightTile = 32;        // k_weights: queries of a tile, keys of a wave
-constexpr int kWeightKeys = 128;       // ... keys of a workgroup
+constexpr int kWeightTile = 32;        // k_weights: queries of a tile, keys of a tile
+constexpr int weight_key_tiles(int d) { return d == 256 ? 1 : 2; }                     // ... tiles of keys of a wave
+constexpr int weight_keys(int d) { return 4 * kWeightTile * weight_key_tiles(d); }     // ... keys of a workgroup
 struct WeightGeom {
     int elem_bytes, d, M, q_len;       // M = queries of a unit: heads that share a KV head, q_len of each
     int n_kv, units, units_per_layer;
