@@ -359,19 +359,20 @@ hipError_t launch_quantize(const SlabTable& rows, const SlabTable& codes, const 
 constexpr int kDequantPieces = 4, kDequantPerWg = 256 * kDequantPieces;   // pieces of 16 codes: of a thread, of a workgroup
 hipError_t launch_dequantize(const SlabTable& codes, const SlabTable& rows, const Q8MoveGeom& g, int slabs, hipStream_t st);
 
-// Angles of the d / 2 rotary pairs: frequencies in quarter turns per row, the rotation that advances a position by kTurnStep rows, and the angles of the rows
-// 0 .. kTurnRows - 1, which turn the seed of a tile's first row into those of all its rows.
+// Angles of the d / 2 rotary pairs: frequencies in quarter turns per row, the rotations that advance a position by kTurnStep rows and by twice as many, and the angles
+// of the rows 0 .. kTurnRows - 1, which turn the seed of a tile's first row into those of all its rows.
 constexpr int kTurnStep = 64, kTurnRows = 32;
 struct TurnTable {
     const double* quarters;            // [d / 2]
     const float2* step;                // [d / 2] (cos, sin)
+    const float2* step2;               // [d / 2]
     const float2* rows;                // [kTurnRows][d / 2]
 };
-constexpr size_t turn_table_bytes(int d) { return (size_t)(d / 2) * (2 + kTurnRows) * 8; }
+constexpr size_t turn_table_bytes(int d) { return (size_t)(d / 2) * (3 + kTurnRows) * 8; }
 inline TurnTable turn_table(const void* at, int d)
 {
     const char* p = (const char*)at;
-    return TurnTable{(const double*)p, (const float2*)(p + d * 4), (const float2*)(p + d * 8)};
+    return TurnTable{(const double*)p, (const float2*)(p + d * 4), (const float2*)(p + d * 8), (const float2*)(p + d * 12)};
 }
 hipError_t launch_turn_table(void* at, int d, double base, hipStream_t st);
 

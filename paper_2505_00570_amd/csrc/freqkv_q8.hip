@@ -236,12 +236,12 @@ __global__ __launch_bounds__(kMoveThreads) void k_dequantize(const Q8MoveGeom, c
 __global__ void k_turn_table(char* at, int d, double base)
 {
     const int i = blockIdx.x * blockDim.x + threadIdx.x, half = d / 2, row = i / half, j = i - row * half;
-    if (row > kTurnRows) return;
+    if (row > kTurnRows + 1) return;
     const double theta = base > 0.0 ? pow(base, -2.0 * (double)j / (double)d) : 0.0;       // no rotary embedding: every angle is zero
     if (row == 0) ((double*)at)[j] = theta * 0.6366197723675814;
-    // row 0: the step; row r + 1: the angle of row r
+    // rows 0 and 1: the steps; row r + 2: the angle of row r
     double s, c;
-    sincos((double)(row ? row - 1 : kTurnStep) * theta, &s, &c);
+    sincos((double)(row == 0 ? kTurnStep : row == 1 ? 2 * kTurnStep : row - 2) * theta, &s, &c);
     ((float2*)(at + d * 4))[row * half + j] = float2{(float)c, (float)s};
 }
 
@@ -250,10 +250,12 @@ namespace {
 constexpr float kSlack = 8.0f;       // log2 of the largest un-rescaled softmax weight (times at most 4 an fp16 operand)
 constexpr int kReseedSteps = 32;     // steps between exact recomputations of the rows' cos/sin
 
-// Byte `ch` of the codes of two rows, as fp16 (exact).
-template <int FMT, int CH> __device__ __forceinline__ half2v pair_of(uint32_t row0, uint32_t row1)
+// Byte CH of the codes of two rows, as fp16 (exact).  RAW, of int8: the byte plus 128, times 2^-24, as the fp16 number that has just it as its bits.
+template <int FMT, int CH, bool RAW> __device__ __forceinline__ half2v pair_of(uint32_t row0, uint32_t row1)
 {
-    if constexpr (FMT == kInt8) {
+    if constexpr (RAW) {
+        return __builtin_bit_cast(half2v, __builtin_amdgcn_perm(row1, row0, 0x0c000c00u | (4u + CH) << 16 | CH));      // (of rows whose bytes are plus 128)
+    } else if constexpr (FMT == kInt8) {
         // (code + 128) behind the byte 0x64 is 1024 + 128 + code in fp16
         const uint32_t u = __builtin_amdgcn_perm(row1, row0, 0x0c000c00u | (4u + CH) << 16 | CH) ^ 0x64806480u;
         return __builtin_bit_cast(half2v, u) - half2v{(_Float16)1152.f, (_Float16)1152.f};
@@ -291,7 +293,7 @@ template <int BANKS> __device__ __forceinline__ uint32_t of_pair(uint32_t x, uin
 //   values     the same instruction, channels x queries over the 32 rows: the weights are, as they lie, the second operand.  They take the block's
 //              scale with them (relative to a power of two that follows the largest, so that fp16 holds them), codes are exact in fp16.
 // cos/sin of a row advance by a fixed rotation of 64 rows per tile from exact seeds, again every kReseedSteps steps (64 such rotations are off by 1e-6 or less).
-// Rows past the end of the chunk are zeros from past the end of a buffer; scores of rows that a query does not see are -inf, their weights zero whatever the scale.
+// Scores of rows that a query does not see are -inf, their weights zero whatever the scale.
 template <int FMT, int D, bool F32, bool ONE>
 __global__ __launch_bounds__(kQ8Waves * 64, (D == 256 || F32 ? 1 : 2))
 void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt, float* __restrict__ part_acc, float* __restrict__ part_ml,
@@ -307,7 +309,9 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
     constexpr bool TIGHT = D == 256;                 // few registers to spare: what need not be at once is kept apart
     typedef typename std::conditional<F32, float, uint16_t>::type T;
 
-    __shared__ float red[W][NQ][D];
+    constexpr int RINGS = W * 2 * 2 * 32 * D, ENDS = W * NQ * D * 4;
+    __shared__ __attribute__((aligned(1024))) char pool[RINGS > ENDS ? RINGS : ENDS];     // rows of two steps, of each wave; then their sums
+    float (*const red)[NQ][D] = (float (*)[NQ][D])pool;
     __shared__ float xm[W][NQ], xl[W][NQ];
     __shared__ half8 qsm[D == 256 && F32 ? 2 * KS : 1][64];
     __shared__ __attribute__((aligned(16))) float2 turns[W][D == 256 ? D : D / 2];
@@ -337,51 +341,85 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
 
     const long long head_off = (long long)b * g.code_batch + (long long)kvh * g.code_head;
     const uint32_t row_bytes = (uint32_t)g.code_token;
-    const int size = nit > 0 ? (int)((uint32_t)(row_end - 1) * row_bytes + (uint32_t)D) : 0;
-    const __amdgpu_buffer_rsrc_t kbuf = __builtin_amdgcn_make_buffer_rsrc((void*)(tab.base[2 * layer] + head_off), 0, size, kBufferFlags);
-    const __amdgpu_buffer_rsrc_t vbuf = __builtin_amdgcn_make_buffer_rsrc((void*)(tab.base[2 * layer + 1] + head_off), 0, size, kBufferFlags);
+    const char* const kbase = tab.base[2 * layer] + head_off;
+    const char* const vbase = tab.base[2 * layer + 1] + head_off;
     const long long scale_off = (long long)layer * g.scale_layer + (long long)b * g.scale_batch + (long long)kvh * g.scale_head;
     const float* const ks = g.k_scale + scale_off;
     const float* const vs = g.v_scale + scale_off;
     const int last_block = max(row_end - 1, 0) >> g.block_shift;
 
-    // ---- rows of a step
-    struct Keys { uint32_t lo[NP][PC / 4], up[NP][PC / 4]; };
-    Keys key[2];
-    uint32_t val[2][4][VW];                          // D = 128: [half][row of the four] as loaded, then [tile][row]
+    // ---- rows of a step, two tiles of 16: copied to the wave's part of LDS two steps ahead, 16 bytes a lane, whole rows side by side.  (Loaded as they are used, with the four
+    // lanes that share a row 16 apart, a load's 64 pieces were 64 requests of the first-level cache.)  Keys lie with their pieces of 16 bytes turned by row, so that lanes that
+    // read the same piece of eight rows find them in different banks.  Rows past the end are the last one's again.
+    constexpr int IN = D / 64, PIECES = D / 16, ROWS = 64 / PIECES;     // copies of a tile, pieces of a row, rows of a copy
+    constexpr int TILE = 16 * D, SLOT = 2 * TILE;
     const int wrow = row0 + 16 * wave;               // first row of the wave's first tile
-    auto words = [&](const __amdgpu_buffer_rsrc_t& buf, uint32_t at, auto& to, auto n) {
-        if constexpr (decltype(n)::value == 4) {
-            const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(buf, at, 0, 0);
-            static_for<4>([&](auto i) { to[i.value] = w[i.value]; });
-        } else if constexpr (decltype(n)::value == 2) {
-            const u32x2 w = __builtin_amdgcn_raw_buffer_load_b64(buf, at, 0, 0);
-            static_for<2>([&](auto i) { to[i.value] = w[i.value]; });
+    char* const keys = pool + wave * 4 * SLOT;       // [slot][tile][row][D]
+    char* const vals = keys + 2 * SLOT;
+    typedef __attribute__((address_space(3))) char* lptr_t;
+    const uint32_t keys_lds = (uint32_t)(uintptr_t)(lptr_t)keys, vals_lds = (uint32_t)(uintptr_t)(lptr_t)vals;
+    auto turned = [](int row, int piece) { return piece ^ (D == 64 ? row >> 1 & 3 : row & 7); };
+    // a lane's copies of a step: where they lie, from the step's first row on (the last step's rows past the end: the last row's again)
+    uint32_t key_at[2 * IN], val_at[2 * IN];
+    static_for<2 * IN>([&](auto i) {
+        const int row = (i.value % IN) * ROWS + lane / PIECES, piece = lane % PIECES;
+        const uint32_t at = (uint32_t)(16 * wave + i.value / IN * kTurnStep + row) * row_bytes;
+        key_at[i.value] = at + (uint32_t)(turned(row, piece) * 16);
+        val_at[i.value] = at + (uint32_t)(piece * 16);
+    });
+    auto ask = [&](int it, uint32_t lds, const char* base, const uint32_t (&at)[2 * IN], auto is_keys) {
+        const int first = row0 + it * kQ8StepRows;
+        const char* const from = base + (uint32_t)first * row_bytes;
+        if (first + kQ8StepRows <= row_end) {
+            static_for<2 * IN>([&](auto i) { lds_dma16(lds + (uint32_t)((it & 1) * SLOT + i.value * 1024), from, at[i.value]); });
         } else {
-            to[0] = __builtin_amdgcn_raw_buffer_load_b32(buf, at, 0, 0);
+            static_for<2 * IN>([&](auto i) {
+                const int r = (i.value % IN) * ROWS + lane / PIECES, piece = lane % PIECES;
+                const int row = min(16 * wave + i.value / IN * kTurnStep + r, row_end - 1 - first);
+                lds_dma16(lds + (uint32_t)((it & 1) * SLOT + i.value * 1024), from,
+                          (uint32_t)row * row_bytes + (uint32_t)((decltype(is_keys)::value ? turned(r, piece) : piece) * 16));
+            });
         }
     };
-    auto load_keys = [&](int it) {
-        static_for<2>([&](auto t) {
-            const uint32_t at = (uint32_t)(wrow + it * kQ8StepRows + t.value * kTurnStep + c) * row_bytes + (uint32_t)(PC * gq);
-            static_for<NP>([&](auto p) {
-                words(kbuf, at + p.value * 4 * PC, key[t.value].lo[p.value], IC<PC / 4>{});
-                words(kbuf, at + D / 2 + p.value * 4 * PC, key[t.value].up[p.value], IC<PC / 4>{});
-            });
+    auto ask_keys = [&](int it) { ask(it, keys_lds, kbase, key_at, IC<1>{}); };
+    auto ask_values = [&](int it) { ask(it, vals_lds, vbase, val_at, IC<0>{}); };
+    auto landed = [](auto n) { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(decltype(n)::value) : "memory"); };      // all copies but the last n
+    auto words = [](const char* p, auto& to, auto n) {
+        if constexpr (decltype(n)::value == 4) {
+            const u32x4 w = *(const u32x4*)p;
+            static_for<4>([&](auto i) { to[i.value] = w[i.value]; });
+        } else if constexpr (decltype(n)::value == 2) {
+            const u32x2 w = *(const u32x2*)p;
+            static_for<2>([&](auto i) { to[i.value] = w[i.value]; });
+        } else {
+            to[0] = *(const uint32_t*)p;
+        }
+    };
+    struct Keys { uint32_t lo[NP][PC / 4], up[NP][PC / 4]; };
+    auto load_keys = [&](const char* tile, Keys& key) {
+        static_for<NP>([&](auto p) {
+            constexpr int HALF = PIECES / 2;
+            if constexpr (PC == 16) {
+                words(tile + c * D + turned(c, gq + 4 * p.value) * 16, key.lo[p.value], IC<4>{});
+                words(tile + c * D + turned(c, HALF + gq + 4 * p.value) * 16, key.up[p.value], IC<4>{});
+            } else {
+                words(tile + c * D + turned(c, gq >> 1) * 16 + (gq & 1) * 8, key.lo[p.value], IC<2>{});
+                words(tile + c * D + turned(c, HALF + (gq >> 1)) * 16 + (gq & 1) * 8, key.up[p.value], IC<2>{});
+            }
         });
     };
-    auto load_values = [&](int it) {
+    uint32_t val[2][4][VW];                          // D = 128: [half][row of the four] as they lie, then [tile][row]
+    auto load_values = [&](const char* slot) {
         if constexpr (D == 128) {
             // 16 bytes a lane, 8 lanes to a row; lanes with 8 in their index have the second tile's rows
-            const uint32_t at = (uint32_t)(wrow + it * kQ8StepRows + (lane >> 3 & 1) * kTurnStep + 4 * gq) * row_bytes + (uint32_t)(16 * (lane & 7));
+            const char* const p = slot + (lane >> 3 & 1) * TILE + 4 * gq * D + 16 * (lane & 7);
             static_for<4>([&](auto r) {
-                const u32x4 w = __builtin_amdgcn_raw_buffer_load_b128(vbuf, at + r.value * row_bytes, 0, 0);
+                const u32x4 w = *(const u32x4*)(p + r.value * D);
                 static_for<2>([&](auto i) { val[0][r.value][i.value] = w[i.value]; val[1][r.value][i.value] = w[2 + i.value]; });
             });
         } else {
             static_for<2>([&](auto t) {
-                const uint32_t at = (uint32_t)(wrow + it * kQ8StepRows + t.value * kTurnStep + 4 * gq) * row_bytes + (uint32_t)(NV * c);
-                static_for<4>([&](auto r) { words(vbuf, at + r.value * row_bytes, val[t.value][r.value], IC<VW>{}); });
+                static_for<4>([&](auto r) { words(slot + t.value * TILE + (4 * gq + r.value) * D + NV * c, val[t.value][r.value], IC<VW>{}); });
             });
         }
     };
@@ -389,11 +427,12 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
     // first channel of the lane `c` of a tile of values: the tile `ct` has the channel ct behind it
     auto channel0 = [](int c) { return D == 128 ? 16 * (c & 7) + 8 * (c >> 3) : NV * c; };
 
-    constexpr bool AHEAD = !(TIGHT && F32);         // a step's rows are asked for in the step before
-    if constexpr (AHEAD) {
-        load_keys(0);
-        load_values(0);
-    }
+    static_for<2>([&](auto i) {
+        if (i.value < nit) {
+            ask_keys(i.value);
+            ask_values(i.value);
+        }
+    });
 
     // ---- the rotary state of the lane's pairs
     float co[HC], si[HC], cd[TIGHT ? 8 : HC], sd[TIGHT ? 8 : HC];
@@ -403,26 +442,31 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
         wave_turns<D>(rt, wrow + it * kQ8StepRows - (cur_len - 1), own, lane);
         static_for<NP>([&](auto p) { seeds<D, PC>(rt, own, c, PC * (gq + 4 * p.value), co + PC * p.value, si + PC * p.value); });
     };
+    // PAIRED: the keys of a step's two tiles turn by the same angle, and the second tile meets queries that are turned back by the rows between them
+    constexpr bool PAIRED = !(TIGHT && F32);
+    const float2* const advance = PAIRED ? rt.step2 : rt.step;
     // (TIGHT: the rotations by a step stay in LDS, each wave has its copy)
-    if constexpr (TIGHT) static_for<D / 128>([&](auto n) { own[D / 2 + n.value * 64 + lane] = rt.step[n.value * 64 + lane]; });
-    else static_for<NP>([&](auto p) { steps<PC>(rt, PC * (gq + 4 * p.value), cd + PC * p.value, sd + PC * p.value); });
+    if constexpr (TIGHT) static_for<D / 128>([&](auto n) { own[D / 2 + n.value * 64 + lane] = advance[n.value * 64 + lane]; });
+    else static_for<NP>([&](auto p) { rotations<PC>(advance + PC * (gq + 4 * p.value), cd + PC * p.value, sd + PC * p.value); });
     seed(0);
 
     // ---- the lane's query c: channels of the group gq, turned by its place less the last one's
     constexpr bool QLDS = TIGHT && F32;              // (in LDS there: all waves have the same)
-    half8 qh[QLDS ? 1 : KS], ql[F32 && !QLDS ? KS : 1];
+    constexpr int SETS = PAIRED ? 2 : 1;
+    half8 qh[SETS][QLDS ? 1 : KS], ql[SETS][F32 && !QLDS ? KS : 1];
     float qfactor;
     {
         float a[HC], bb[HC], most = 0.f;
         const T* const qp = (const T*)q + (head0 + min(c, queries - 1)) * D;
-        static_for<HC>([&](auto i) {
-            const int ch = pair_index(i.value);
-            float x, y;
-            if constexpr (F32) { x = qp[ch]; y = qp[D / 2 + ch]; }
-            else { x = __uint_as_float((uint32_t)qp[ch] << 16); y = __uint_as_float((uint32_t)qp[D / 2 + ch] << 16); }
-            a[i.value] = x;
-            bb[i.value] = y;
-            most = fmaxf(most, fmaxf(fabsf(x), fabsf(y)));
+        constexpr int N = 16 / (int)sizeof(T);        // channels to 16 bytes
+        static_for<HC / N>([&](auto i) {
+            const u32x4 x = *(const u32x4*)(qp + pair_index(i.value * N)), y = *(const u32x4*)(qp + D / 2 + pair_index(i.value * N));
+            static_for<N>([&](auto j) {
+                constexpr int to = i.value * N + j.value;
+                a[to] = __uint_as_float(F32 ? x[j.value % 4] : j.value & 1 ? x[j.value / 2] & 0xffff0000u : x[j.value / 2] << 16);
+                bb[to] = __uint_as_float(F32 ? y[j.value % 4] : j.value & 1 ? y[j.value / 2] & 0xffff0000u : y[j.value / 2] << 16);
+                most = fmaxf(most, fmaxf(fabsf(a[to]), fabsf(bb[to])));
+            });
         });
         most = fold<32>(fold<16>(most, Max{}), Max{});
         const int e = max(-110, min(exponent_of(most), 126)) - 6;        // largest element -> 2^6 .. 2^7
@@ -438,20 +482,34 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
                 if constexpr (i.value % 4 == 3) __builtin_amdgcn_sched_barrier(0);        // (all at once, they take more registers than there are)
             });
         }
-        static_for<KS>([&](auto k) {
-            half8 hi, lo;
-            static_for<8>([&](auto i) {
-                constexpr int at = k.value % (KS / 2) * 8 + i.value;
-                const float x = k.value < KS / 2 ? a[at] : bb[at];
-                hi[i.value] = (_Float16)x;
-                lo[i.value] = (_Float16)(x - (float)(_Float16)x);
-            });
-            if constexpr (QLDS) {
-                if (wave == k.value % W) { qsm[k.value][lane] = hi; qsm[KS + k.value][lane] = lo; }
-            } else {
-                qh[k.value] = hi;
-                if constexpr (F32) ql[k.value] = lo;
+        static_for<SETS>([&](auto set) {
+            if constexpr (set.value > 0) {
+                static_for<NP>([&](auto p) {
+                    float sc[PC], ss[PC];
+                    rotations<PC>(rt.step + PC * (gq + 4 * p.value), sc, ss);
+                    static_for<PC>([&](auto i) {
+                        constexpr int at = PC * p.value + i.value;
+                        const float x = a[at], y = bb[at];
+                        a[at] = fmaf(x, sc[i.value], y * ss[i.value]);
+                        bb[at] = fmaf(y, sc[i.value], -(x * ss[i.value]));
+                    });
+                });
             }
+            static_for<KS>([&](auto k) {
+                half8 hi, lo;
+                static_for<8>([&](auto i) {
+                    constexpr int at = k.value % (KS / 2) * 8 + i.value;
+                    const float x = k.value < KS / 2 ? a[at] : bb[at];
+                    hi[i.value] = (_Float16)x;
+                    lo[i.value] = (_Float16)(x - (float)(_Float16)x);
+                });
+                if constexpr (QLDS) {
+                    if (wave == k.value % W) { qsm[k.value][lane] = hi; qsm[KS + k.value][lane] = lo; }
+                } else {
+                    qh[set.value][k.value] = hi;
+                    if constexpr (F32) ql[set.value][k.value] = lo;
+                }
+            });
         });
         if constexpr (QLDS) lds_barrier();
     }
@@ -459,10 +517,18 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
     float m = kMinusBig, lsum = 0.f, vref = 0.f;     // vref: the power of two that the sums are relative to
     f32x4 acc[NV];
     static_for<NV>([&](auto ct) { acc[ct.value] = f32x4{0.f, 0.f, 0.f, 0.f}; });
+    // RAW: int8 codes go to the matrix cores as bytes plus 128, times 2^-24 (the numbers below fp16's normal ones: no conversion), and what the 128 add to each sum, the weights' sum times
+    // 128, is added up beside.  Fp32 queries would lose two of their bits by the difference.
+    constexpr bool RAW = FMT == kInt8 && !F32;
+    f32x4 off = {0.f, 0.f, 0.f, 0.f};
 
     for (int it = 0; it < nit; ++it) {
         if (it > 0 && it % kReseedSteps == 0) seed(it);
-        if constexpr (!AHEAD) load_keys(it);
+        constexpr int N = 2 * IN;                        // copies of a step's keys, and of its values
+        // behind the step's keys were asked for: its values, and keys and values of the next step
+        if (it + 1 < nit) landed(IC<3 * N>{});
+        else landed(IC<N>{});
+        const char* const kslot = keys + (it & 1) * SLOT;
         const float kscale[2] = {ks[block_of(it, 0)], ks[block_of(it, 1)]};
         const float vscale[2] = {vs[block_of(it, 0)], vs[block_of(it, 1)]};
         // ---- scores
@@ -472,9 +538,11 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
         f32x4 sc[2];
         static_for<2>([&](auto t) {
             sc[t.value] = f32x4{0.f, 0.f, 0.f, 0.f};
+            Keys key;
+            load_keys(kslot + t.value * TILE, key);
             static_for<KS / 2>([&](auto k) {             // eight pairs: a k-step of the lower half and one of the upper
                 half8 kh[2], kl[2];
-                if constexpr (TIGHT) {
+                if constexpr (TIGHT && (!PAIRED || t.value == 1)) {
                     static_for<4>([&](auto n) {
                         const f32x4 w = *(const f32x4*)(own + D / 2 + PC * ((int)(ln >> 4) + 4 * (8 * k.value / PC)) + (8 * k.value + 2 * n.value) % PC);
                         cd[2 * n.value] = w[0]; sd[2 * n.value] = w[1];
@@ -485,20 +553,22 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
                     constexpr int i = 8 * k.value + 2 * n.value, w = i / 4;
                     if constexpr (n.value % 2 == 0) {
                         if constexpr (TIGHT) {
-                            here(key[t.value].lo[w / (PC / 4)][w % (PC / 4)]);
-                            here(key[t.value].up[w / (PC / 4)][w % (PC / 4)]);
+                            here(key.lo[w / (PC / 4)][w % (PC / 4)]);
+                            here(key.up[w / (PC / 4)][w % (PC / 4)]);
                         }
-                        values_of<FMT>(key[t.value].lo[w / (PC / 4)][w % (PC / 4)], ka);
-                        values_of<FMT>(key[t.value].up[w / (PC / 4)][w % (PC / 4)], kb);
+                        values_of<FMT>(key.lo[w / (PC / 4)][w % (PC / 4)], ka);
+                        values_of<FMT>(key.up[w / (PC / 4)][w % (PC / 4)], kb);
                     }
                     float lo[2], up[2];
                     static_for<2>([&](auto o) {
                         constexpr int j = 2 * (n.value % 2) + o.value, at = i + o.value, by = TIGHT ? at % 8 : at;
                         lo[o.value] = fmaf(ka[j], co[at], -(kb[j] * si[at]));
                         up[o.value] = fmaf(kb[j], co[at], ka[j] * si[at]);
-                        const float cn = fmaf(co[at], cd[by], -(si[at] * sd[by]));
-                        si[at] = fmaf(si[at], cd[by], co[at] * sd[by]);
-                        co[at] = cn;
+                        if constexpr (!PAIRED || t.value == 1) {
+                            const float cn = fmaf(co[at], cd[by], -(si[at] * sd[by]));
+                            si[at] = fmaf(si[at], cd[by], co[at] * sd[by]);
+                            co[at] = cn;
+                        }
                     });
                     const half2v l = halves(lo[0], lo[1]), u = halves(up[0], up[1]);
                     kh[0][2 * n.value] = l[0]; kh[0][2 * n.value + 1] = l[1];
@@ -513,7 +583,7 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
                     constexpr int at = k.value + h.value * (KS / 2);
                     half8 qa, qb;
                     if constexpr (QLDS) { qa = qsm[at][ln]; qb = qsm[KS + at][ln]; }
-                    else { qa = qh[at]; if constexpr (F32) qb = ql[at]; }
+                    else { qa = qh[PAIRED ? t.value : 0][at]; if constexpr (F32) qb = ql[PAIRED ? t.value : 0][at]; }
                     if constexpr (F32) {
                         sc[t.value] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl[h.value], qa, sc[t.value], 0, 0, 0);
                         sc[t.value] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh[h.value], qb, sc[t.value], 0, 0, 0);
@@ -523,18 +593,19 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
                 if constexpr (TIGHT) apart();
             });
         });
-        if (AHEAD && it + 1 < nit) load_keys(it + 1);
-        if constexpr (!AHEAD) load_values(it);
-        const int step0 = row0 + it * kQ8StepRows;
-        const bool tail = step0 + kQ8StepRows > seen;
-        bool hidden[2][4];
-        static_for<2>([&](auto t) {
-            const float f = kscale[t.value] * qfactor;
-            static_for<4>([&](auto r) {
-                hidden[t.value][r.value] = tail && wrow + it * kQ8StepRows + t.value * kTurnStep + 4 * gq + r.value >= limit;
-                sc[t.value][r.value] = hidden[t.value][r.value] ? -INFINITY : sc[t.value][r.value] * f;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (read, before they are written again)
+        if (it + 2 < nit) ask_keys(it + 2);
+        static_for<2>([&](auto t) { sc[t.value] *= kscale[t.value] * qfactor; });
+        // rows that not all queries see: which of the lane's (bit 4 t + r) its query does not
+        const bool tail = row0 + (it + 1) * kQ8StepRows > seen;
+        uint32_t hidden = 0;
+        if (tail) {
+            static_for<8>([&](auto i) {
+                const bool no = wrow + it * kQ8StepRows + i.value / 4 * kTurnStep + 4 * gq + i.value % 4 >= limit;
+                hidden |= no ? 1u << i.value : 0u;
+                sc[i.value / 4][i.value % 4] = no ? -INFINITY : sc[i.value / 4][i.value % 4];
             });
-        });
+        }
         // ---- softmax: the reference point m only moves when a score exceeds it by more than 2^kSlack
         float mx = fmaxf(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[0][2], sc[0][3])), fmaxf(fmaxf(sc[1][0], sc[1][1]), fmaxf(sc[1][2], sc[1][3])));
         mx = fold<32>(fold<16>(mx, Max{}), Max{});
@@ -544,26 +615,37 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
             m = mn;
             lsum *= f;
             static_for<NV>([&](auto ct) { acc[ct.value] *= f; });
+            if constexpr (RAW) off *= f;
         }
         const float larger = fmaxf(vscale[0], vscale[1]);
         if (larger > 4.f * vref && larger < INFINITY) {
             const float to = __uint_as_float(__float_as_uint(larger) & 0x7f800000u), f = vref / to;
             vref = to;
             static_for<NV>([&](auto ct) { acc[ct.value] *= f; });
+            if constexpr (RAW) off *= f;
         }
         const float per = vref > 0.f ? 1.f / vref : 0.f;
         half8 ph, pl;
-        static_for<2>([&](auto t) {
-            const float v = vscale[t.value] * per;
-            static_for<4>([&](auto r) {
-                const float p = exp2_fast(sc[t.value][r.value] - m);
-                lsum += p;
-                const float x = hidden[t.value][r.value] ? 0.f : p * v;
-                ph[4 * t.value + r.value] = (_Float16)x;
-                if constexpr (F32) pl[4 * t.value + r.value] = (_Float16)(x - (float)(_Float16)x);
-            });
+        float x[8];
+        static_for<8>([&](auto i) {
+            const float p = exp2_fast(sc[i.value / 4][i.value % 4] - m);
+            lsum += p;
+            x[i.value] = p * (vscale[i.value / 4] * per);
         });
-        // ---- values
+        if (tail) static_for<8>([&](auto i) { x[i.value] = hidden >> i.value & 1 ? 0.f : x[i.value]; });      // (a scale may be NaN)
+        static_for<4>([&](auto i) {
+            const half2v h = halves(x[2 * i.value], x[2 * i.value + 1]);
+            ph[2 * i.value] = h[0]; ph[2 * i.value + 1] = h[1];
+            if constexpr (F32) {
+                const half2v l = halves(x[2 * i.value] - (float)h[0], x[2 * i.value + 1] - (float)h[1]);
+                pl[2 * i.value] = l[0]; pl[2 * i.value + 1] = l[1];
+            }
+        });
+        // ---- values: behind them were asked for keys and values of the next step, and keys of the one after
+        if (it + 2 < nit) landed(IC<3 * N>{});
+        else if (it + 1 < nit) landed(IC<2 * N>{});
+        else landed(IC<0>{});
+        load_values(vals + (it & 1) * SLOT);
         if constexpr (D == 128) {
             // (as loaded: [lower or upper 8 channels][row])  Lanes 8 apart have the same 16 channels of the two tiles: after the exchange each has half of the channels of both.
             static_for<4>([&](auto r) {
@@ -574,13 +656,19 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
                 });
             });
         }
+        if constexpr (RAW) {
+            static_for<8>([&](auto r) { static_for<VW>([&](auto w) { val[r.value / 4][r.value % 4][w.value] ^= 0x80808080u; }); });
+            half8 offset;
+            static_for<8>([&](auto i) { offset[i.value] = __builtin_bit_cast(_Float16, (uint16_t)128); });
+            off = __builtin_amdgcn_mfma_f32_16x16x32_f16(offset, ph, off, 0, 0, 0);
+        }
         static_for<VW>([&](auto w) {
             if constexpr (TIGHT) static_for<8>([&](auto r) { here(val[r.value / 4][r.value % 4][w.value]); });
             static_for<4>([&](auto ch) {
                 half8 a;
                 static_for<4>([&](auto r) {
                     constexpr int t = r.value / 2, n = r.value % 2 * 2;
-                    const half2v x = pair_of<FMT, ch.value>(val[t][n][w.value], val[t][n + 1][w.value]);
+                    const half2v x = pair_of<FMT, ch.value, RAW>(val[t][n][w.value], val[t][n + 1][w.value]);
                     a[2 * r.value] = x[0];
                     a[2 * r.value + 1] = x[1];
                 });
@@ -590,7 +678,8 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
             });
             if constexpr (TIGHT) apart();
         });
-        if (AHEAD && it + 1 < nit) load_values(it + 1);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (it + 2 < nit) ask_values(it + 2);
     }
 
     // ---- the waves' states: common reference point, sums, results of the chunk
@@ -601,8 +690,12 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
     static_for<W - 1>([&](auto w) { M = fmaxf(M, xm[w.value + 1][c]); });
     const float f = exp2_fast(m - M);
     if (gq == 0) xl[wave][c] = lsum * f;
+    const float ends = f * vref;
     static_for<NV>([&](auto ct) {
-        static_for<4>([&](auto r) { red[wave][c][channel0(4 * gq + r.value) + ct.value] = acc[ct.value][r.value] * (f * vref); });
+        static_for<4>([&](auto r) {
+            const float x = RAW ? (acc[ct.value][r.value] - off[r.value]) * 16777216.f : acc[ct.value][r.value];
+            red[wave][c][channel0(4 * gq + r.value) + ct.value] = x * ends;
+        });
     });
     lds_barrier();
     for (int idx = threadIdx.x; idx < queries * (D / 2); idx += W * 64) {
@@ -668,7 +761,7 @@ hipError_t launch_dequantize(const SlabTable& codes, const SlabTable& rows, cons
 
 hipError_t launch_turn_table(void* at, int d, double base, hipStream_t st)
 {
-    hipLaunchKernelGGL(k_turn_table, dim3((unsigned)((1 + kTurnRows) * (d / 2) + 255) / 256), dim3(256), 0, st, (char*)at, d, base);
+    hipLaunchKernelGGL(k_turn_table, dim3((unsigned)((2 + kTurnRows) * (d / 2) + 255) / 256), dim3(256), 0, st, (char*)at, d, base);
     return hipGetLastError();
 }
 

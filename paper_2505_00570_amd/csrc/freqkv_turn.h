@@ -57,11 +57,11 @@ template <int D, int N> __device__ __forceinline__ void seeds(const TurnTable& t
         });
     });
 }
-// The rotations by kTurnStep rows of N adjacent pairs.
-template <int N> __device__ __forceinline__ void steps(const TurnTable& t, int pair, float* c, float* s)
+// N adjacent pairs (N even) of a table of rotations.
+template <int N> __device__ __forceinline__ void rotations(const float2* from, float* c, float* s)
 {
     static_for<N / 2>([&](auto i) {
-        const f32x4 w = *(const f32x4*)(t.step + pair + 2 * i.value);
+        const f32x4 w = *(const f32x4*)(from + 2 * i.value);
         c[2 * i.value] = w[0]; s[2 * i.value] = w[1];
         c[2 * i.value + 1] = w[2]; s[2 * i.value + 1] = w[3];
     });

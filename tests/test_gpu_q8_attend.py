@@ -144,7 +144,7 @@ def test_less_workspace_is_fewer_chunks():
     q, k8, v8, scales = _case(1, 1, 1, 4, 2000, 1, 128, torch.float32, "int8", 64, 5)
     lens = torch.full((1,), 2000, dtype=torch.int32, device=DEV)
     k, v = (ref.values(c[:, :, :, :2000], s, 64) for c, s in zip((k8, v8), scales))
-    for ws in (34816, 34816 + 5 * (4 * 128 * 4 + 32) + 256):
+    for ws in (35840, 35840 + 5 * (4 * 128 * 4 + 32) + 256):
         out, lse = _attend(q, k8, v8, scales, 64, 2000, workspace=ws)
         _check(q, None, None, None, 64, lens, BASE, out, lse, (k, v))
 

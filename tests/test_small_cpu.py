@@ -125,4 +125,4 @@ def test_plans():
                     assert p.flops == 4.0 * d * seen * 6 * 6
                     assert p.bytes_algorithmic == 12 * (2 * cur * d + 2 * 3 * n * d * (2 if dt == fk.BF16 else 4))
                 _, p = fk.attend_weights_plan(L, 6, 2, d, cur, n)
-                assert p.flops == 2.0 * d * seen * 6 * 6 and p.workspace_bytes >= 34816
+                assert p.flops == 2.0 * d * seen * 6 * 6 and p.workspace_bytes >= 35840
