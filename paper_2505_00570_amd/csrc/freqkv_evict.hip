@@ -106,8 +106,8 @@ void k_weights_few(const WeightGeom, const T* __restrict__ q, const float* __res
     float co[HP][8], si[HP][8];
     float2* const own = turns[wave];
     auto seed = [&](int n) {
-        wave_turns<D>(rt, wrow + n * kTurnStep - (cur_len - 1), own, lane);
-        static_for<HP>([&](auto p) { seeds<D, 8>(rt, own, c, 32 * p.value + 8 * gq, co[p.value], si[p.value]); });
+        wave_turns<D>(rt.quarters, wrow + n * kTurnStep - (cur_len - 1), own, lane);
+        static_for<HP>([&](auto p) { seeds<D, 8>(rt.rows, own, c, 32 * p.value + 8 * gq, co[p.value], si[p.value]); });
     };
     static_for<(D / 2 + 63) / 64>([&](auto n) { if (n.value * 64 + lane < D / 2) own[D / 2 + n.value * 64 + lane] = rt.step[n.value * 64 + lane]; });
     seed(0);
@@ -258,7 +258,7 @@ void k_weights(const WeightGeom, const _Float16* __restrict__ operands, const fl
             read8(kbuf, at + p.value * 16 * (uint32_t)sizeof(T), lo[p.value]);
             read8(kbuf, at + (D / 2 + p.value * 16) * (uint32_t)sizeof(T), up[p.value]);
         });
-        wave_turns<D>(rt, first - (cur_len - 1), own, lane);
+        wave_turns<D>(rt.quarters, first - (cur_len - 1), own, lane);
         static_for<HP>([&](auto p) {
             static_for<8>([&](auto i) {
                 // (of finite values: a row that is not keeps to itself)
@@ -270,7 +270,7 @@ void k_weights(const WeightGeom, const _Float16* __restrict__ operands, const fl
         kfactor[kt.value] = pw.up;
         static_for<HP>([&](auto p) {
             float x[8], y[8], tc[8], ts[8];
-            seeds<D, 8>(rt, own, l32, 16 * p.value + 8 * hw, tc, ts);
+            seeds<D, 8>(rt.rows, own, l32, 16 * p.value + 8 * hw, tc, ts);
             static_for<8>([&](auto i) {
                 const float l = at8<i.value>(lo[p.value]) * pw.down, u = at8<i.value>(up[p.value]) * pw.down;
                 x[i.value] = fmaf(l, tc[i.value], -(u * ts[i.value]));

@@ -360,7 +360,8 @@ constexpr int kDequantPieces = 4, kDequantPerWg = 256 * kDequantPieces;   // pie
 hipError_t launch_dequantize(const SlabTable& codes, const SlabTable& rows, const Q8MoveGeom& g, int slabs, hipStream_t st);
 
 // Angles of the d / 2 rotary pairs: frequencies in quarter turns per row, the rotations that advance a position by kTurnStep rows and by twice as many, and the angles
-// of the rows 0 .. kTurnRows - 1, which turn the seed of a tile's first row into those of all its rows.
+// of the rows 0 .. kTurnRows - 1, which turn the seed of a tile's first row into those of all its rows.  All in one piece, in this order; a row's pieces of two pairs lie
+// turned by the row (piece ^ (row & 7)), so that they are in different banks once in LDS.
 constexpr int kTurnStep = 64, kTurnRows = 32;
 struct TurnTable {
     const double* quarters;            // [d / 2]

@@ -242,7 +242,8 @@ __global__ void k_turn_table(char* at, int d, double base)
     // rows 0 and 1: the steps; row r + 2: the angle of row r
     double s, c;
     sincos((double)(row == 0 ? kTurnStep : row == 1 ? 2 * kTurnStep : row - 2) * theta, &s, &c);
-    ((float2*)(at + d * 4))[row * half + j] = float2{(float)c, (float)s};
+    const int place = row < 2 ? j : 2 * ((j / 2) ^ ((row - 2) & 7)) + j % 2;
+    ((float2*)(at + d * 4))[row * half + place] = float2{(float)c, (float)s};
 }
 
 namespace {
@@ -296,7 +297,7 @@ template <int BANKS> __device__ __forceinline__ uint32_t of_pair(uint32_t x, uin
 // Scores of rows that a query does not see are -inf, their weights zero whatever the scale.
 template <int FMT, int D, bool F32, bool ONE>
 __global__ __launch_bounds__(kQ8Waves * 64, (D == 256 || F32 ? 1 : 2))
-void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt, float* __restrict__ part_acc, float* __restrict__ part_ml,
+void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable tables, float* __restrict__ part_acc, float* __restrict__ part_ml,
                  void* __restrict__ out, float* __restrict__ lse, const SlabTable tab)
 {
     const Q8AttGeom g = first_argument<decltype(k_attend_q8<FMT, D, F32, ONE>)>();
@@ -309,12 +310,14 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
     constexpr bool TIGHT = D == 256;                 // few registers to spare: what need not be at once is kept apart
     typedef typename std::conditional<F32, float, uint16_t>::type T;
 
-    constexpr int RINGS = W * 2 * 2 * 32 * D, ENDS = W * NQ * D * 4;
-    __shared__ __attribute__((aligned(1024))) char pool[RINGS > ENDS ? RINGS : ENDS];     // rows of two steps, of each wave; then their sums
-    float (*const red)[NQ][D] = (float (*)[NQ][D])pool;
+    constexpr int SLOTS = TIGHT && F32 ? 1 : 2;      // steps whose rows LDS holds
+    constexpr int RINGS = W * SLOTS * 2 * 32 * D, RED = D + 4, ENDS = W * NQ * RED * 4, TABLES = (3 + 16) * (D / 2) * 8;
+    __shared__ __attribute__((aligned(1024))) char pool[RINGS > ENDS ? RINGS : ENDS];     // rows of SLOTS steps, of each wave; then their sums
+    __shared__ __attribute__((aligned(1024))) char tsm[(TABLES + 1023) / 1024 * 1024];    // the start of the tables: frequencies, rotations by a step, 16 rows
+    float (*const red)[NQ][RED] = (float (*)[NQ][RED])pool;      // (four more to a row: queries in different banks)
     __shared__ float xm[W][NQ], xl[W][NQ];
     __shared__ half8 qsm[D == 256 && F32 ? 2 * KS : 1][64];
-    __shared__ __attribute__((aligned(16))) float2 turns[W][D == 256 ? D : D / 2];
+    __shared__ __attribute__((aligned(16))) float2 turns[W][D / 2];
 
     const int lane = threadIdx.x & 63, c = lane & 15, gq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -354,10 +357,10 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
     constexpr int IN = D / 64, PIECES = D / 16, ROWS = 64 / PIECES;     // copies of a tile, pieces of a row, rows of a copy
     constexpr int TILE = 16 * D, SLOT = 2 * TILE;
     const int wrow = row0 + 16 * wave;               // first row of the wave's first tile
-    char* const keys = pool + wave * 4 * SLOT;       // [slot][tile][row][D]
-    char* const vals = keys + 2 * SLOT;
+    char* const ring = pool + wave * SLOTS * 2 * SLOT;       // [slot][keys, values][tile][row][D]
     typedef __attribute__((address_space(3))) char* lptr_t;
-    const uint32_t keys_lds = (uint32_t)(uintptr_t)(lptr_t)keys, vals_lds = (uint32_t)(uintptr_t)(lptr_t)vals;
+    const uint32_t ring_lds = (uint32_t)(uintptr_t)(lptr_t)ring;
+    auto slot_of = [](int it) { return SLOTS == 2 ? (it & 1) * 2 * SLOT : 0; };
     auto turned = [](int row, int piece) { return piece ^ (D == 64 ? row >> 1 & 3 : row & 7); };
     // a lane's copies of a step: where they lie, from the step's first row on (the last step's rows past the end: the last row's again)
     uint32_t key_at[2 * IN], val_at[2 * IN];
@@ -371,18 +374,18 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
         const int first = row0 + it * kQ8StepRows;
         const char* const from = base + (uint32_t)first * row_bytes;
         if (first + kQ8StepRows <= row_end) {
-            static_for<2 * IN>([&](auto i) { lds_dma16(lds + (uint32_t)((it & 1) * SLOT + i.value * 1024), from, at[i.value]); });
+            static_for<2 * IN>([&](auto i) { lds_dma16(lds + (uint32_t)(slot_of(it) + i.value * 1024), from, at[i.value]); });
         } else {
             static_for<2 * IN>([&](auto i) {
                 const int r = (i.value % IN) * ROWS + lane / PIECES, piece = lane % PIECES;
                 const int row = min(16 * wave + i.value / IN * kTurnStep + r, row_end - 1 - first);
-                lds_dma16(lds + (uint32_t)((it & 1) * SLOT + i.value * 1024), from,
+                lds_dma16(lds + (uint32_t)(slot_of(it) + i.value * 1024), from,
                           (uint32_t)row * row_bytes + (uint32_t)((decltype(is_keys)::value ? turned(r, piece) : piece) * 16));
             });
         }
     };
-    auto ask_keys = [&](int it) { ask(it, keys_lds, kbase, key_at, IC<1>{}); };
-    auto ask_values = [&](int it) { ask(it, vals_lds, vbase, val_at, IC<0>{}); };
+    auto ask_keys = [&](int it) { ask(it, ring_lds, kbase, key_at, IC<1>{}); };
+    auto ask_values = [&](int it) { ask(it, ring_lds + SLOT, vbase, val_at, IC<0>{}); };
     auto landed = [](auto n) { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(decltype(n)::value) : "memory"); };      // all copies but the last n
     auto words = [](const char* p, auto& to, auto n) {
         if constexpr (decltype(n)::value == 4) {
@@ -427,27 +430,45 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
     // first channel of the lane `c` of a tile of values: the tile `ct` has the channel ct behind it
     auto channel0 = [](int c) { return D == 128 ? 16 * (c & 7) + 8 * (c >> 3) : NV * c; };
 
-    static_for<2>([&](auto i) {
-        if (i.value < nit) {
-            ask_keys(i.value);
-            ask_values(i.value);
-        }
+    // ---- the start: tables, a fourth of them each wave, and queries, each wave its own, in the last slot; then the rows of the first step.  All are copies: what came back to
+    // registers would be awaited with all copies asked for before it, which for the first rows, asked for by all workgroups at once, are microseconds.
+    constexpr int N = 2 * IN;                        // copies of a step's keys, and of its values
+    constexpr int QB = D * (int)sizeof(T), QPIECES = QB / 16, QROWS = 64 / QPIECES, QIN = NQ / QROWS;    // of a query; copies of all
+    char* const qraw = ring + (SLOTS - 1) * 2 * SLOT;
+    static_assert(NQ * QB <= 2 * SLOT, "a slot holds the queries");
+    constexpr int TIN = (TABLES + 1023) / 1024;
+    static_for<(TIN + W - 1) / W>([&](auto i) {
+        const int part = i.value * W + wave;
+        if (part < TIN) lds_dma16((uint32_t)(uintptr_t)(lptr_t)tsm + (uint32_t)part * 1024, tables.quarters, (uint32_t)(part * 1024 + lane * 16));
     });
+    static_for<QIN>([&](auto i) {
+        const int r = i.value * QROWS + lane / QPIECES, piece = (lane % QPIECES) ^ (r & 7);
+        lds_dma16(ring_lds + (uint32_t)((SLOTS - 1) * 2 * SLOT + i.value * 1024), (const char*)q + head0 * QB, (uint32_t)(min(r, queries - 1) * QB + piece * 16));
+    });
+    if (SLOTS == 2 && nit > 0) {
+        ask_keys(0);
+        ask_values(0);
+        landed(IC<2 * N>{});
+    } else {
+        landed(IC<0>{});
+    }
+    lds_barrier();
+    const struct { const double* quarters; const float2 *step, *step2, *rows; } rt = {(const double*)tsm, (const float2*)(tsm + D * 4), (const float2*)(tsm + D * 8),
+                                                                                   (const float2*)(tsm + D * 12)};
 
     // ---- the rotary state of the lane's pairs
     float co[HC], si[HC], cd[TIGHT ? 8 : HC], sd[TIGHT ? 8 : HC];
     auto pair_index = [&](int i) { return PC * (gq + 4 * (i / PC)) + i % PC; };
     float2* const own = turns[wave];
     auto seed = [&](int it) {
-        wave_turns<D>(rt, wrow + it * kQ8StepRows - (cur_len - 1), own, lane);
-        static_for<NP>([&](auto p) { seeds<D, PC>(rt, own, c, PC * (gq + 4 * p.value), co + PC * p.value, si + PC * p.value); });
+        wave_turns<D>(rt.quarters, wrow + it * kQ8StepRows - (cur_len - 1), own, lane);
+        static_for<NP>([&](auto p) { seeds<D, PC>(rt.rows, own, c, PC * (gq + 4 * p.value), co + PC * p.value, si + PC * p.value); });
     };
     // PAIRED: the keys of a step's two tiles turn by the same angle, and the second tile meets queries that are turned back by the rows between them
     constexpr bool PAIRED = !(TIGHT && F32);
     const float2* const advance = PAIRED ? rt.step2 : rt.step;
-    // (TIGHT: the rotations by a step stay in LDS, each wave has its copy)
-    if constexpr (TIGHT) static_for<D / 128>([&](auto n) { own[D / 2 + n.value * 64 + lane] = advance[n.value * 64 + lane]; });
-    else static_for<NP>([&](auto p) { rotations<PC>(advance + PC * (gq + 4 * p.value), cd + PC * p.value, sd + PC * p.value); });
+    // (TIGHT: the rotations by a step stay in LDS)
+    if constexpr (!TIGHT) static_for<NP>([&](auto p) { rotations<PC>(advance + PC * (gq + 4 * p.value), cd + PC * p.value, sd + PC * p.value); });
     seed(0);
 
     // ---- the lane's query c: channels of the group gq, turned by its place less the last one's
@@ -457,12 +478,12 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
     float qfactor;
     {
         float a[HC], bb[HC], most = 0.f;
-        const T* const qp = (const T*)q + (head0 + min(c, queries - 1)) * D;
-        constexpr int N = 16 / (int)sizeof(T);        // channels to 16 bytes
-        static_for<HC / N>([&](auto i) {
-            const u32x4 x = *(const u32x4*)(qp + pair_index(i.value * N)), y = *(const u32x4*)(qp + D / 2 + pair_index(i.value * N));
-            static_for<N>([&](auto j) {
-                constexpr int to = i.value * N + j.value;
+        constexpr int CH = 16 / (int)sizeof(T);       // channels to 16 bytes
+        static_for<HC / CH>([&](auto i) {
+            const int piece = pair_index(i.value * CH) / CH;
+            const u32x4 x = *(const u32x4*)(qraw + c * QB + (piece ^ (c & 7)) * 16), y = *(const u32x4*)(qraw + c * QB + ((QPIECES / 2 + piece) ^ (c & 7)) * 16);
+            static_for<CH>([&](auto j) {
+                constexpr int to = i.value * CH + j.value;
                 a[to] = __uint_as_float(F32 ? x[j.value % 4] : j.value & 1 ? x[j.value / 2] & 0xffff0000u : x[j.value / 2] << 16);
                 bb[to] = __uint_as_float(F32 ? y[j.value % 4] : j.value & 1 ? y[j.value / 2] & 0xffff0000u : y[j.value / 2] << 16);
                 most = fmaxf(most, fmaxf(fabsf(a[to]), fabsf(bb[to])));
@@ -514,6 +535,12 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
         if constexpr (QLDS) lds_barrier();
     }
 
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // (queries read, before rows are written there)
+    if (SLOTS == 2 && nit > 1) {
+        ask_keys(1);
+        ask_values(1);
+    }
+
     float m = kMinusBig, lsum = 0.f, vref = 0.f;     // vref: the power of two that the sums are relative to
     f32x4 acc[NV];
     static_for<NV>([&](auto ct) { acc[ct.value] = f32x4{0.f, 0.f, 0.f, 0.f}; });
@@ -524,11 +551,17 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
 
     for (int it = 0; it < nit; ++it) {
         if (it > 0 && it % kReseedSteps == 0) seed(it);
-        constexpr int N = 2 * IN;                        // copies of a step's keys, and of its values
         // behind the step's keys were asked for: its values, and keys and values of the next step
-        if (it + 1 < nit) landed(IC<3 * N>{});
-        else landed(IC<N>{});
-        const char* const kslot = keys + (it & 1) * SLOT;
+        if constexpr (SLOTS == 1) {
+            ask_keys(it);
+            ask_values(it);
+            landed(IC<N>{});
+        } else if (it + 1 < nit) {
+            landed(IC<3 * N>{});
+        } else {
+            landed(IC<N>{});
+        }
+        const char* const kslot = ring + slot_of(it);
         const float kscale[2] = {ks[block_of(it, 0)], ks[block_of(it, 1)]};
         const float vscale[2] = {vs[block_of(it, 0)], vs[block_of(it, 1)]};
         // ---- scores
@@ -544,7 +577,7 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
                 half8 kh[2], kl[2];
                 if constexpr (TIGHT && (!PAIRED || t.value == 1)) {
                     static_for<4>([&](auto n) {
-                        const f32x4 w = *(const f32x4*)(own + D / 2 + PC * ((int)(ln >> 4) + 4 * (8 * k.value / PC)) + (8 * k.value + 2 * n.value) % PC);
+                        const f32x4 w = *(const f32x4*)(advance + PC * ((int)(ln >> 4) + 4 * (8 * k.value / PC)) + (8 * k.value + 2 * n.value) % PC);
                         cd[2 * n.value] = w[0]; sd[2 * n.value] = w[1];
                         cd[2 * n.value + 1] = w[2]; sd[2 * n.value + 1] = w[3];
                     });
@@ -594,7 +627,7 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
             });
         });
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (read, before they are written again)
-        if (it + 2 < nit) ask_keys(it + 2);
+        if (SLOTS == 2 && it + 2 < nit) ask_keys(it + 2);
         static_for<2>([&](auto t) { sc[t.value] *= kscale[t.value] * qfactor; });
         // rows that not all queries see: which of the lane's (bit 4 t + r) its query does not
         const bool tail = row0 + (it + 1) * kQ8StepRows > seen;
@@ -642,10 +675,10 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
             }
         });
         // ---- values: behind them were asked for keys and values of the next step, and keys of the one after
-        if (it + 2 < nit) landed(IC<3 * N>{});
-        else if (it + 1 < nit) landed(IC<2 * N>{});
+        if (SLOTS == 2 && it + 2 < nit) landed(IC<3 * N>{});
+        else if (SLOTS == 2 && it + 1 < nit) landed(IC<2 * N>{});
         else landed(IC<0>{});
-        load_values(vals + (it & 1) * SLOT);
+        load_values(kslot + SLOT);
         if constexpr (D == 128) {
             // (as loaded: [lower or upper 8 channels][row])  Lanes 8 apart have the same 16 channels of the two tiles: after the exchange each has half of the channels of both.
             static_for<4>([&](auto r) {
@@ -679,7 +712,7 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
             if constexpr (TIGHT) apart();
         });
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        if (it + 2 < nit) ask_values(it + 2);
+        if (SLOTS == 2 && it + 2 < nit) ask_values(it + 2);
     }
 
     // ---- the waves' states: common reference point, sums, results of the chunk
@@ -691,12 +724,18 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable rt
     const float f = exp2_fast(m - M);
     if (gq == 0) xl[wave][c] = lsum * f;
     const float ends = f * vref;
-    static_for<NV>([&](auto ct) {
-        static_for<4>([&](auto r) {
-            const float x = RAW ? (acc[ct.value][r.value] - off[r.value]) * 16777216.f : acc[ct.value][r.value];
-            red[wave][c][channel0(4 * gq + r.value) + ct.value] = x * ends;
+    if (c < queries) {
+        static_for<NV / 4>([&](auto ct) {
+            static_for<4>([&](auto r) {
+                f32x4 x;
+                static_for<4>([&](auto i) {
+                    const float y = acc[4 * ct.value + i.value][r.value];
+                    x[i.value] = (RAW ? (y - off[r.value]) * 16777216.f : y) * ends;
+                });
+                *(f32x4*)&red[wave][c][channel0(4 * gq + r.value) + 4 * ct.value] = x;
+            });
         });
-    });
+    }
     lds_barrier();
     for (int idx = threadIdx.x; idx < queries * (D / 2); idx += W * 64) {
         const int j = idx / (D / 2), ch = 2 * (idx - j * (D / 2));

@@ -34,22 +34,22 @@ __device__ __forceinline__ CosSin turn(double quarters, int pos)
 }
 
 // cos and sin of a position common to the wave, of all pairs, to the wave's own part of LDS (a wave's LDS instructions take effect in order).
-template <int D> __device__ __forceinline__ void wave_turns(const TurnTable& t, int pos, float2* own, int lane)
+template <int D> __device__ __forceinline__ void wave_turns(const double* quarters, int pos, float2* own, int lane)
 {
     static_for<(D / 2 + 63) / 64>([&](auto n) {
         const int j = n.value * 64 + lane;
         if (D / 2 >= 64 || j < D / 2) {
-            const CosSin x = turn(t.quarters[j], pos);
+            const CosSin x = turn(quarters[j], pos);
             own[j] = float2{x.c, x.s};
         }
     });
     asm volatile("" ::: "memory");
 }
 // ... times those of a row from there on, of N adjacent pairs (N even): the lane's seeds
-template <int D, int N> __device__ __forceinline__ void seeds(const TurnTable& t, const float2* own, int row, int pair, float* c, float* s)
+template <int D, int N> __device__ __forceinline__ void seeds(const float2* rows, const float2* own, int row, int pair, float* c, float* s)
 {
     static_for<N / 2>([&](auto i) {
-        const f32x4 w = *(const f32x4*)(own + pair + 2 * i.value), r = *(const f32x4*)(t.rows + row * (D / 2) + pair + 2 * i.value);
+        const f32x4 w = *(const f32x4*)(own + pair + 2 * i.value), r = *(const f32x4*)(rows + row * (D / 2) + 2 * ((pair / 2 + i.value) ^ (row & 7)));
         static_for<2>([&](auto n) {
             constexpr int k = 2 * n.value;
             c[2 * i.value + n.value] = fmaf(w[k], r[k], -(w[k + 1] * r[k + 1]));
