@@ -1911,7 +1911,8 @@ freqkv_status_t check_weights(const freqkv_layout_t* L, int n_q, int n_kv, int d
     w.M = (int)M;
     w.workspace_bytes = kTableBytes;
     if (w.M <= kWeightFew) {
-        const long long most = (cur_len + kTurnStep - 1) / kTurnStep, ns = std::min(most, std::max(1LL, 1024 / w.units));
+        const long long most = (cur_len + kTurnStep - 1) / kTurnStep, least = (cur_len + kWeightFewChunk - 1) / kWeightFewChunk;
+        const long long ns = std::min(most, std::max(least, 512 / w.units));
         w.chunk = (int)round_up((cur_len + ns - 1) / ns, kTurnStep);
         w.n_chunk = (cur_len + w.chunk - 1) / w.chunk;
         if (w.units * w.n_chunk >= 1 << 23) return FREQKV_E_UNSUPPORTED;

@@ -58,6 +58,14 @@ __device__ __forceinline__ void split8(const float (&x)[8], half8& hi, half8& lo
     });
 }
 
+// Sums of two values over lanes O apart: the lanes without O in their index get that of x, the others that of y.
+template <int O> __device__ __forceinline__ float halved(float x, float y)
+{
+    const auto s = O == 16 ? __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false)
+                           : __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
 __device__ __forceinline__ void pin(half8& x) { asm volatile("" : "+v"(x) :: "memory"); }
 
 // log2(e) times a query's lse, to be taken from its scores.  One that saw no row (-inf) adds nothing.
@@ -65,17 +73,27 @@ __device__ __forceinline__ float taken(float lse) { return lse == -INFINITY ? IN
 
 }  // namespace
 
-// Up to 16 queries: bound by the rows.  A wave has tiles of 16 rows; a lane (c, g) = (lane & 15, lane >> 4) has of row c the channels 32 p + 8 g .. + 7 for every p,
-// so that a rotary pair is in one lane, and gets the scores of row c with the queries 4 g .. 4 g + 3.  v_mfma_f32_16x16x4_f32: products and sums in fp32, nothing to split (with
-// keys and queries as sums of two fp16 a tile took 390 vector instructions instead of 190: 16 sequences of 4096 to 8192 rows, 8 KV heads, 76 us).
-template <typename T, int D>
-__global__ __launch_bounds__(256, (D == 256 ? 1 : sizeof(T) == 4 ? 2 : 3))
-void k_weights_few(const WeightGeom, const T* __restrict__ q, const float* __restrict__ lse, const TurnTable rt, float* __restrict__ weights,
+// Up to 16 queries: bound by the rows.  A wave has tiles of 16 rows, kTurnStep apart; a lane (c, g) = (lane & 15, lane >> 4) has of row c the channels 32 p + 8 g .. + 7 for every p,
+// so that a rotary pair is in one lane.  Products and sums are fp32 (with keys and queries as sums of two fp16 a tile took 390 vector instructions instead of 190):
+//   SETS 1, 2   up to four or eight queries: v_mfma_f32_4x4x1_16b_f32, a quad of lanes' four rows times the queries that the lanes' places in the quad name, a product of each
+//               channel group; sums over the groups by exchanges that halve the rows, to one score of each set to a lane
+//   SETS 0      up to 16: v_mfma_f32_16x16x4_f32, to the scores of row c with the queries 4 g .. 4 g + 3; four times as long on the matrix cores as a set
+// Tiles are copied to LDS, SLOTS of them under way for each wave, a row's pieces of 16 bytes
+// turned by the row, and their weights stay there to the end, when all of the chunk's are written, or added to what is there, together: with rows in registers a tile ahead, and weights
+// added as they came, 16 sequences of 4096 to 8192 rows of 8 KV heads took 78 us.
+template <typename T, int D, int SETS>
+__global__ __launch_bounds__(256, (D == 256 || sizeof(T) == 4 ? 1 : 2))
+void k_weights_few(const WeightGeom, const T* __restrict__ q, const float* __restrict__ lse, const TurnTable tables, float* __restrict__ weights,
                    const SlabTable tab)
 {
-    const WeightGeom g = first_argument<decltype(k_weights_few<T, D>)>();
+    const WeightGeom g = first_argument<decltype(k_weights_few<T, D, SETS>)>();
     constexpr int HP = D / 64;                      // pieces of eight channels of a lane in each half
-    __shared__ __attribute__((aligned(16))) float2 turns[4][D];       // of each wave: where seeds come from, and the rotations by a step
+    constexpr int RB = D * (int)sizeof(T), PIECES = RB / 16, TILE = 16 * RB, N = TILE / 1024, ROWS = 16 / N;      // bytes, pieces of 16 of a row; copies of a tile, rows of one
+    constexpr int SLOTS = D == 256 && sizeof(T) == 4 ? 2 : 3, TABLES = (3 + 16) * (D / 2) * 8, TIN = (TABLES + 1023) / 1024;
+    __shared__ __attribute__((aligned(1024))) char pool[4][SLOTS][TILE];
+    __shared__ __attribute__((aligned(1024))) char tsm[TIN * 1024];       // the start of the tables: frequencies, rotations by a step, 16 rows
+    __shared__ __attribute__((aligned(16))) float2 turns[4][D / 2];
+    __shared__ float sums[kWeightFewChunk];
     const int lane = threadIdx.x & 63, c = lane & 15, gq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int unit = g.by_chunk.quotient(blockIdx.x), ck = blockIdx.x - unit * g.n_chunk;
@@ -87,64 +105,110 @@ void k_weights_few(const WeightGeom, const T* __restrict__ q, const float* __res
     if (row0 >= row_end) return;
     const uint32_t row_bytes = (uint32_t)g.stride_token * (uint32_t)sizeof(T);
     const char* const kbase = tab.base[layer] + ((long long)b * g.stride_batch + (long long)kvh * g.stride_head) * (long long)sizeof(T);
-    const __amdgpu_buffer_rsrc_t kbuf = __builtin_amdgcn_make_buffer_rsrc((void*)kbase, 0, (int)((uint32_t)(row_end - 1) * row_bytes + (uint32_t)(D * sizeof(T))), kBufferFlags);
-    float* const wout = weights + (long long)unit * g.capacity;
-
     const int wrow = row0 + 16 * wave, tiles = wrow < row_end ? (row_end - wrow + kTurnStep - 1) / kTurnStep : 0;
-    Eight<T> lo[HP], up[HP];
-    float old = 0.f;                                 // of the weight that the lane writes
-    auto load = [&](int n) {
-        const int row = wrow + n * kTurnStep + c;
-        const uint32_t at = (uint32_t)row * row_bytes + (uint32_t)(8 * gq) * (uint32_t)sizeof(T);
-        static_for<HP>([&](auto p) {
-            read8(kbuf, at + p.value * 32 * (uint32_t)sizeof(T), lo[p.value]);
-            read8(kbuf, at + (D / 2 + p.value * 32) * (uint32_t)sizeof(T), up[p.value]);
+    const long long head0 = (long long)unit * g.M;
+
+    // ---- copies: tables, a fourth of them each wave, and queries, each wave its own, in the last slot; then the first tiles
+    typedef __attribute__((address_space(3))) char* lptr_t;
+    const uint32_t ring = (uint32_t)(uintptr_t)(lptr_t)&pool[wave][0][0];
+    const int crow = lane / PIECES;                 // row of a copy; its piece is turned by the row of the tile
+    auto piece_at = [&](auto i) { return (uint32_t)(((lane % PIECES) ^ ((i.value * ROWS + crow) & 7)) * 16); };
+    auto ask = [&](int n) {
+        const int first = wrow + n * kTurnStep;
+        const char* const from = kbase + (uint32_t)first * row_bytes;
+        static_for<N>([&](auto i) {                 // (past the end: the last row again)
+            const int row = min(i.value * ROWS + crow, row_end - 1 - first);
+            lds_dma16(ring + (uint32_t)(n % SLOTS * TILE + i.value * 1024), from, (uint32_t)row * row_bytes + piece_at(i));
         });
-        if (g.accumulate) old = wout[min(row, row_end - 1)];
     };
-    load(0);
+    auto landed = [](auto n) { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(decltype(n)::value) : "memory"); };      // all copies but the last n
+    static_for<(TIN + 3) / 4>([&](auto i) {
+        const int part = i.value * 4 + wave;
+        if (part < TIN) lds_dma16((uint32_t)(uintptr_t)(lptr_t)tsm + (uint32_t)part * 1024, tables.quarters, (uint32_t)(part * 1024 + lane * 16));
+    });
+    static_for<N>([&](auto i) {
+        lds_dma16(ring + (uint32_t)((SLOTS - 1) * TILE + i.value * 1024), (const char*)(q + head0 * D), (uint32_t)(min(i.value * ROWS + crow, g.M - 1) * RB) + piece_at(i));
+    });
+    if (tiles > 0) ask(0);
+    if (SLOTS == 3 && tiles > 1) {
+        ask(1);
+        landed(IC<2 * N>{});
+    } else if (tiles > 0) {
+        landed(IC<N>{});
+    } else {
+        landed(IC<0>{});
+    }
+    lds_barrier();
+    const double* const quarters = (const double*)tsm;
+    const float2 *const step = (const float2*)(tsm + D * 4), *const rows = (const float2*)(tsm + D * 12);
+
     float co[HP][8], si[HP][8];
     float2* const own = turns[wave];
     auto seed = [&](int n) {
-        wave_turns<D>(rt.quarters, wrow + n * kTurnStep - (cur_len - 1), own, lane);
-        static_for<HP>([&](auto p) { seeds<D, 8>(rt.rows, own, c, 32 * p.value + 8 * gq, co[p.value], si[p.value]); });
+        wave_turns<D>(quarters, wrow + n * kTurnStep - (cur_len - 1), own, lane);
+        static_for<HP>([&](auto p) { seeds<D, 8>(rows, own, c, 32 * p.value + 8 * gq, co[p.value], si[p.value]); });
     };
-    static_for<(D / 2 + 63) / 64>([&](auto n) { if (n.value * 64 + lane < D / 2) own[D / 2 + n.value * 64 + lane] = rt.step[n.value * 64 + lane]; });
     seed(0);
+    // eight channels of a row of a tile
+    auto eight = [&](const char* tile, int row, int channel, Eight<T>& x) {
+        const int piece = channel * (int)sizeof(T) / 16;
+        const char* const at = tile + row * RB;
+        x.a = *(const u32x4*)(at + (piece ^ (row & 7)) * 16);
+        if constexpr (sizeof(T) == 4) x.b = *(const u32x4*)(at + ((piece + 1) ^ (row & 7)) * 16);
+    };
 
-    // ---- queries: the lane's is c, scaled by log2(e) / sqrt(d), turned by its place less the last one's; of those that its scores are of, lse and last rows
-    float ql[HP][8], qu[HP][8];
-    const long long head0 = (long long)unit * g.M;
-    const int mine = min(c, g.M - 1), place = mine - g.by_q.quotient(mine) * g.q_len;
-    {
-        const T* const qp = q + (head0 + mine) * D + 8 * gq;
+    // ---- the lane's queries (of each set lane & 3, or c), scaled by log2(e) / sqrt(d), turned by their places less the last one's; of those that its scores are of, lse and last rows
+    constexpr int NQ = SETS ? SETS : 1;
+    float ql[NQ][HP][8], qu[NQ][HP][8];
+    auto place_of = [&](int j) { return j - g.by_q.quotient(j) * g.q_len; };
+    static_for<NQ>([&](auto set) {
+        constexpr int Q = set.value;
+        const int mine = min(SETS ? 4 * Q + (lane & 3) : c, g.M - 1), place = place_of(mine);
         static_for<HP>([&](auto p) {
             Eight<T> a, bb;
-            read8(qp + 32 * p.value, a);
-            read8(qp + D / 2 + 32 * p.value, bb);
-            static_for<8>([&](auto i) { ql[p.value][i.value] = at8<i.value>(a) * g.qscale; qu[p.value][i.value] = at8<i.value>(bb) * g.qscale; });
+            eight(&pool[wave][SLOTS - 1][0], mine, 32 * p.value + 8 * gq, a);
+            eight(&pool[wave][SLOTS - 1][0], mine, D / 2 + 32 * p.value + 8 * gq, bb);
+            static_for<8>([&](auto i) { ql[Q][p.value][i.value] = at8<i.value>(a) * g.qscale; qu[Q][p.value][i.value] = at8<i.value>(bb) * g.qscale; });
             if (g.q_len > 1) {
                 static_for<8>([&](auto i) {
-                    const float l = ql[p.value][i.value], u = qu[p.value][i.value];
-                    const CosSin t = turn(rt.quarters[32 * p.value + 8 * gq + i.value], place + 1 - g.q_len);
-                    ql[p.value][i.value] = fmaf(l, t.c, -(u * t.s));
-                    qu[p.value][i.value] = fmaf(u, t.c, l * t.s);
+                    const float l = ql[Q][p.value][i.value], u = qu[Q][p.value][i.value];
+                    const CosSin t = turn(quarters[32 * p.value + 8 * gq + i.value], place + 1 - g.q_len);
+                    ql[Q][p.value][i.value] = fmaf(l, t.c, -(u * t.s));
+                    qu[Q][p.value][i.value] = fmaf(u, t.c, l * t.s);
                     if constexpr (i.value % 4 == 3) __builtin_amdgcn_sched_barrier(0);    // (all at once, they take more registers than there are)
                 });
             }
         });
-    }
-    const float taken_mine = c < g.M ? taken(lse[head0 + mine]) : INFINITY;      // (no query there: nothing is added)
-    float less[4];
-    int last[4];                                     // row of the query
-    static_for<4>([&](auto r) {
-        less[r.value] = __shfl(taken_mine, 4 * gq + r.value);
-        last[r.value] = cur_len - g.q_len + __shfl(place, 4 * gq + r.value);
     });
+    constexpr int NS = SETS ? SETS : 4;
+    float less[NS];
+    int last[NS];                                    // row of the query
+    static_for<NS>([&](auto r) {
+        // (of a query that there is not nothing is added; by scalar loads, which do not queue behind the copies)
+        less[r.value] = INFINITY;
+        static_for<4>([&](auto of) {
+            const int j = SETS ? 4 * r.value + of.value : 4 * of.value + r.value;
+            const float x = j < g.M ? taken(lse[head0 + j]) : INFINITY;
+            less[r.value] = (SETS ? lane & 3 : gq) == of.value ? x : less[r.value];
+        });
+        last[r.value] = cur_len - g.q_len + place_of(min(SETS ? 4 * r.value + (lane & 3) : 4 * gq + r.value, g.M - 1));
+    });
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // (queries read, before rows are written there)
+    if (tiles > SLOTS - 1) ask(SLOTS - 1);
 
     for (int n = 0; n < tiles; ++n) {
         if (n > 0 && n % 64 == 0) seed(n);
-        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+        if (SLOTS == 3 && n + 2 < tiles) landed(IC<2 * N>{});
+        else if (n + 1 < tiles) landed(IC<N>{});
+        else landed(IC<0>{});
+        const char* const tile = &pool[wave][n % SLOTS][0];
+        Eight<T> lo[HP], up[HP];
+        static_for<HP>([&](auto p) {
+            eight(tile, c, 32 * p.value + 8 * gq, lo[p.value]);
+            eight(tile, c, D / 2 + 32 * p.value + 8 * gq, up[p.value]);
+        });
+        f32x4 s[NQ];
+        static_for<NQ>([&](auto set) { s[set.value] = f32x4{0.f, 0.f, 0.f, 0.f}; });
         int ln = lane;
         asm volatile("" : "+v"(ln));                 // (rotations are read in every step, and not kept in registers from before the loop)
         static_for<HP>([&](auto p) {
@@ -152,25 +216,46 @@ void k_weights_few(const WeightGeom, const T* __restrict__ q, const float* __res
                 constexpr int P = p.value, I = i.value;
                 const float l = at8<I>(lo[P]), u = at8<I>(up[P]);
                 const float x = fmaf(l, co[P][I], -(u * si[P][I])), y = fmaf(u, co[P][I], l * si[P][I]);
-                const float2 by = own[D / 2 + 32 * P + 8 * (ln >> 4) + I];
+                const float2 by = step[32 * P + 8 * (ln >> 4) + I];
                 const float cn = fmaf(co[P][I], by.x, -(si[P][I] * by.y));
                 si[P][I] = fmaf(si[P][I], by.x, co[P][I] * by.y);
                 co[P][I] = cn;
-                s = __builtin_amdgcn_mfma_f32_16x16x4f32(ql[P][I], x, s, 0, 0, 0);
-                s = __builtin_amdgcn_mfma_f32_16x16x4f32(qu[P][I], y, s, 0, 0, 0);
+                if constexpr (SETS == 0) {
+                    s[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(ql[0][P][I], x, s[0], 0, 0, 0);
+                    s[0] = __builtin_amdgcn_mfma_f32_16x16x4f32(qu[0][P][I], y, s[0], 0, 0, 0);
+                } else {
+                    static_for<NQ>([&](auto set) { s[set.value] = __builtin_amdgcn_mfma_f32_4x4x1f32(x, ql[set.value][P][I], s[set.value], 0, 0, 0); });
+                    static_for<NQ>([&](auto set) { s[set.value] = __builtin_amdgcn_mfma_f32_4x4x1f32(y, qu[set.value][P][I], s[set.value], 0, 0, 0); });
+                }
             });
         });
-        const float before = old;
-        if (n + 1 < tiles) load(n + 1);
-        const int row = wrow + n * kTurnStep + c;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (read, before it is written again)
+        if (n + SLOTS < tiles) ask(n + SLOTS);
         float w = 0.f;
-        static_for<4>([&](auto r) {
-            const float e = exp2_fast(s[r.value] - less[r.value]);
-            w += row <= last[r.value] ? e : 0.f;
-        });
-        w = fold<32>(fold<16>(w, Add{}), Add{});
-        if (gq == 0 && row < row_end) wout[row] = before + w;
+        if constexpr (SETS == 0) {
+            const int row = wrow + n * kTurnStep + c;
+            static_for<4>([&](auto r) {
+                const float e = exp2_fast(s[0][r.value] - less[r.value]);
+                w += row <= last[r.value] ? e : 0.f;
+            });
+            w = fold<32>(fold<16>(w, Add{}), Add{});
+            if (gq == 0) sums[row - row0] = w;
+        } else {
+            // the lane's row is the g-th of its quad's four
+            const int row = wrow + n * kTurnStep + (c & 12) + gq;
+            static_for<NQ>([&](auto set) {
+                const float score = halved<32>(halved<16>(s[set.value][0], s[set.value][1]), halved<16>(s[set.value][2], s[set.value][3]));
+                const float e = exp2_fast(score - less[set.value]);
+                w += row <= last[set.value] ? e : 0.f;
+            });
+            w += dpp<0xB1>(w);
+            w += dpp<0x4E>(w);
+            if ((lane & 3) == 0) sums[row - row0] = w;
+        }
     }
+    lds_barrier();
+    float* const wout = weights + (long long)unit * g.capacity;
+    for (int r = row0 + (int)threadIdx.x; r < row_end; r += 256) wout[r] = g.accumulate ? wout[r] + sums[r - row0] : sums[r - row0];
 }
 
 // Queries as operands: a workgroup has a tile of 32, eight threads to a query.
@@ -631,11 +716,15 @@ template <class F> static hipError_t by_type(const WeightGeom& g, F&& f)
 
 hipError_t launch_weights_few(const SlabTable& tab, const WeightGeom& g, const void* q, const float* lse, const TurnTable& rt, float* weights, hipStream_t st)
 {
-    if (g.M < 1 || g.M > kWeightFew || g.n_chunk < 1 || g.chunk % kTurnStep || (long long)g.n_chunk * g.chunk < g.cur_len) return hipErrorInvalidValue;
+    if (g.M < 1 || g.M > kWeightFew || g.n_chunk < 1 || g.chunk % kTurnStep || g.chunk > kWeightFewChunk || (long long)g.n_chunk * g.chunk < g.cur_len) return hipErrorInvalidValue;
     return by_type(g, [&](auto t, auto d) {
         typedef decltype(t) T;
-        hipLaunchKernelGGL((k_weights_few<T, decltype(d)::value>), dim3((unsigned)(g.units * g.n_chunk)), dim3(256), 0, st, g, (const T*)q, lse, rt, weights, tab);
-        return hipGetLastError();
+        auto launch = [&](auto sets) {
+            hipLaunchKernelGGL((k_weights_few<T, decltype(d)::value, decltype(sets)::value>), dim3((unsigned)(g.units * g.n_chunk)), dim3(256), 0, st, g, (const T*)q, lse, rt,
+                               weights, tab);
+            return hipGetLastError();
+        };
+        return g.M <= 4 ? launch(IC<1>{}) : g.M <= 8 ? launch(IC<2>{}) : launch(IC<0>{});
     });
 }
 

@@ -400,7 +400,7 @@ hipError_t launch_attend_q8(const SlabTable& tab, const Q8AttGeom& g, const void
                             float* lse, hipStream_t st);
 
 // ---- attention weights of the cached rows, and eviction by them -----------------------------------------
-constexpr int kWeightFew = 16;         // queries of a unit that k_weights_few takes
+constexpr int kWeightFew = 16, kWeightFewChunk = 2048;     // queries of a unit that k_weights_few takes, rows of a workgroup at most
 constexpr int kWeightTile = 32;        // k_weights: queries of a tile, keys of a tile
 constexpr int weight_key_tiles(int d) { return d == 256 ? 1 : 2; }                     // ... tiles of keys of a wave
 constexpr int weight_keys(int d) { return 4 * kWeightTile * weight_key_tiles(d); }     // ... keys of a workgroup
