@@ -1895,7 +1895,7 @@ struct WeightShape {
     AttShape a;
     long long units;                    // of a pass
     int M, n_chunk, chunk, q_tiles, n_split, split_tiles, key_blocks;
-    size_t off_factors, off_parts, workspace_bytes;
+    size_t off_parts, workspace_bytes;
 };
 
 freqkv_status_t check_weights(const freqkv_layout_t* L, int n_q, int n_kv, int d, int cur_len, int q_len, WeightShape* out)
@@ -1924,8 +1924,7 @@ freqkv_status_t check_weights(const freqkv_layout_t* L, int n_q, int n_kv, int d
         w.split_tiles = (int)((w.q_tiles + ns - 1) / ns);
         w.n_split = (w.q_tiles + w.split_tiles - 1) / w.split_tiles;
         if (wgs * w.n_split >= 1 << 23 || w.units * w.q_tiles >= 1 << 23) return FREQKV_E_UNSUPPORTED;
-        w.off_factors = kTableBytes + (size_t)w.units * w.q_tiles * weight_operand_bytes(d);
-        w.off_parts = w.off_factors + (size_t)w.units * w.q_tiles * kWeightTile * sizeof(float2);
+        w.off_parts = kTableBytes + (size_t)w.units * w.q_tiles * weight_operand_bytes(d);
         w.workspace_bytes = w.off_parts + (w.n_split > 1 ? (size_t)w.n_split * w.units * cur_len * sizeof(float) : 0);
     }
     *out = w;
@@ -2104,8 +2103,8 @@ freqkv_status_t freqkv_attend_weights(const void* q, const void* k, const float*
         if (w.M <= kWeightFew) {
             HIP_TRY(launch_weights_few(tab, g, qp, lse + head0, rt, to, st));
         } else {
-            HIP_TRY(launch_weights_queries(g, qp, lse + head0, rt, ws + kTableBytes, (float2*)(ws + w.off_factors), st));
-            HIP_TRY(launch_weights(tab, g, ws + kTableBytes, (const float2*)(ws + w.off_factors), rt, (float*)(ws + w.off_parts), to, st));
+            HIP_TRY(launch_weights_queries(g, qp, lse + head0, rt, ws + kTableBytes, st));
+            HIP_TRY(launch_weights(tab, g, ws + kTableBytes, rt, (float*)(ws + w.off_parts), to, st));
         }
     }
     return FREQKV_OK;

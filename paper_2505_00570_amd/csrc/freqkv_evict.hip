@@ -261,7 +261,7 @@ void k_weights_few(const WeightGeom, const T* __restrict__ q, const float* __res
 // Queries as operands: a workgroup has a tile of 32, eight threads to a query.
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_weights_queries(const WeightGeom, const T* __restrict__ q, const float* __restrict__ lse, const TurnTable rt,
-                                                         _Float16* __restrict__ operands, float2* __restrict__ factors)
+                                                         char* __restrict__ operands)
 {
     const WeightGeom g = first_argument<decltype(k_weights_queries<T, D>)>();
     constexpr int N = D / 16;                       // pairs of a thread
@@ -286,7 +286,8 @@ __global__ __launch_bounds__(256) void k_weights_queries(const WeightGeom, const
     most = fmaxf(most, dpp<0x4E>(most));
     most = fmaxf(most, dpp<0x141>(most));
     const Power pw = power_for(most);
-    _Float16* const to = operands + ((long long)unit * g.q_tiles + tile) * (2 * kWeightTile * D);
+    char* const block = operands + ((long long)unit * g.q_tiles + tile) * weight_operand_bytes(D);
+    _Float16* const to = (_Float16*)block;
     static_for<N>([&](auto i) {
         const int ch = N * sub + i.value;
         const float l = a[i.value] * pw.down, u = bb[i.value] * pw.down;
@@ -300,20 +301,27 @@ __global__ __launch_bounds__(256) void k_weights_queries(const WeightGeom, const
             p[kWeightTile * D] = (_Float16)(xy[n.value] - (float)h);
         });
     });
-    if (sub == 0) factors[((long long)unit * g.q_tiles + tile) * kWeightTile + j] = float2{there ? pw.up * g.qscale : 0.f, there ? -taken(lse[head]) : -INFINITY};
+    if (sub == 0) ((float2*)(block + 4 * kWeightTile * D))[j] = float2{there ? pw.up * g.qscale : 0.f, there ? -taken(lse[head]) : -INFINITY};
 }
 
 // More queries: bound by the matrix cores.  A wave has KT tiles of 32 keys, in registers; v_mfma_f32_32x32x16_f16, keys x queries, so that a lane has one query's
 // scores with 16 keys of a tile: its lse and factor are one number each, and weights add up, over all queries, without an exchange until the end.  A tile of queries, 16 KB
-// at d = 128, comes from the L2 once for each wave; two tiles of keys use it twice (one: 2.0 TB/s asked of the first-level cache, which is what it gives).
+// at d = 128, is copied to LDS once for the workgroup's four waves, two tiles ahead, and each wave uses it for two tiles of keys.  (Keys loaded to registers, 16 bytes a lane of 32
+// rows, with their angles from memory, and queries for each wave from the L2: 64 queries on 4 x 8192 rows, 8 KV heads of 4, 75 us.)
 template <typename T, int D>
 __global__ __launch_bounds__(256, (D == 256 ? 1 : 2))
-void k_weights(const WeightGeom, const _Float16* __restrict__ operands, const float2* __restrict__ factors, const TurnTable rt,
-               float* __restrict__ parts, float* __restrict__ weights, const SlabTable tab)
+void k_weights(const WeightGeom, const _Float16* __restrict__ operands, const TurnTable tables, float* __restrict__ parts, float* __restrict__ weights, const SlabTable tab)
 {
     const WeightGeom g = first_argument<decltype(k_weights<T, D>)>();
     constexpr int KS = D / 16, HP = KS / 2, KT = weight_key_tiles(D), KEYS = kWeightTile * KT;         // k-steps; of a half; keys of a wave
+    constexpr int RB = D * (int)sizeof(T), PIECES = RB / 16, KTILE = kWeightTile * RB, KN = KTILE / 1024, ROWS = kWeightTile / KN;      // of a tile of keys as it is cached
+    constexpr int QTILE = 4 * kWeightTile * D, QN = QTILE / 4096, SLOTS = 3;       // of a tile of queries; copies of it by each wave
+    constexpr int TABLES = (3 + kWeightTile) * (D / 2) * 8, TIN = (TABLES + 1023) / 1024;
     static_assert(kWeightTile <= kTurnRows, "rows of a tile");
+    constexpr bool STAGED = 4 * KTILE <= SLOTS * QTILE;                     // keys of 16 bits by way of LDS; of 32 there is no room for them
+    __shared__ __attribute__((aligned(1024))) char pool[SLOTS * QTILE];       // a tile of keys of each wave, then tiles of queries
+    __shared__ __attribute__((aligned(1024))) char tsm[TIN * 1024];       // the start of the tables: frequencies, rotations by a step, 32 rows
+    __shared__ __attribute__((aligned(256))) float2 fsm[4][SLOTS][kWeightTile];
     __shared__ __attribute__((aligned(16))) float2 turns[4][D / 2];
     const int lane = threadIdx.x & 63, l32 = lane & 31, hw = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -324,26 +332,60 @@ void k_weights(const WeightGeom, const _Float16* __restrict__ operands, const fl
     const int b = g.by_kv.quotient(rem), kvh = rem - b * g.n_kv;
     int cur_len = g.cur_len;
     if (g.cur_lens) cur_len = max(0, min(g.cur_lens[b], g.cur_len));
-    const int row0 = (kb * 4 + wave) * KEYS;
-    if (row0 >= cur_len) return;
+    const int first_row = kb * 4 * KEYS, row0 = first_row + wave * KEYS;
+    if (first_row >= cur_len) return;
     const uint32_t row_bytes = (uint32_t)g.stride_token * (uint32_t)sizeof(T);
     const char* const kbase = tab.base[layer] + ((long long)b * g.stride_batch + (long long)kvh * g.stride_head) * (long long)sizeof(T);
-    const __amdgpu_buffer_rsrc_t kbuf = __builtin_amdgcn_make_buffer_rsrc((void*)kbase, 0, (int)((uint32_t)(cur_len - 1) * row_bytes + (uint32_t)(D * sizeof(T))), kBufferFlags);
 
-    // ---- keys, turned by their position less the last row's, divided by a power of two common to a tile
+    // ---- keys: a tile of each wave at a time, through LDS a row's pieces of 16 bytes turned by the row
+    typedef __attribute__((address_space(3))) char* lptr_t;
+    auto landed = [](auto n) { asm volatile("s_waitcnt vmcnt(%0)" :: "n"(decltype(n)::value) : "memory"); };      // all copies but the last n
+    const char* const own_tile = pool + wave * KTILE;
+    auto ask_keys = [&](int kt) {
+        if constexpr (!STAGED) return;
+        const int first = row0 + kt * kWeightTile;
+        static_for<KN>([&](auto i) {                // (past the end: the last row again)
+            const int r = i.value * ROWS + lane / PIECES, row = min(first + r, cur_len - 1);
+            lds_dma16((uint32_t)(uintptr_t)(lptr_t)(pool + wave * KTILE) + (uint32_t)(i.value * 1024), kbase,
+                      (uint32_t)row * row_bytes + (uint32_t)(((lane % PIECES) ^ (r & 7)) * 16));
+        });
+    };
+    static_for<(TIN + 3) / 4>([&](auto i) {
+        const int part = i.value * 4 + wave;
+        if (part < TIN) lds_dma16((uint32_t)(uintptr_t)(lptr_t)tsm + (uint32_t)part * 1024, tables.quarters, (uint32_t)(part * 1024 + lane * 16));
+    });
+    ask_keys(0);
+    landed(IC<0>{});
+    lds_barrier();
+    const double* const quarters = (const double*)tsm;
+    const float2* const rows = (const float2*)(tsm + D * 12);
+
+    // turned by their position less the last row's, divided by a power of two common to a tile
     half8 kh[KT][KS], kl[KT][KS];
     float kfactor[KT];
     float2* const own = turns[wave];
     static_for<KT>([&](auto kt) {
         const int first = row0 + kt.value * kWeightTile;
         Eight<T> lo[HP], up[HP];
-        const uint32_t at = (uint32_t)(first + l32) * row_bytes + (uint32_t)(8 * hw) * (uint32_t)sizeof(T);
         float most = 0.f;
+        auto eight = [&](int channel, Eight<T>& x) {
+            if constexpr (!STAGED) {
+                const char* const from = kbase + (uint32_t)min(first + l32, cur_len - 1) * row_bytes + channel * (int)sizeof(T);
+                x.a = *(const u32x4*)from;
+                if constexpr (sizeof(T) == 4) x.b = *(const u32x4*)(from + 16);
+                return;
+            }
+            const int piece = channel * (int)sizeof(T) / 16;
+            x.a = *(const u32x4*)(own_tile + l32 * RB + (piece ^ (l32 & 7)) * 16);
+        };
+        if constexpr (STAGED && kt.value > 0) landed(IC<0>{});
         static_for<HP>([&](auto p) {
-            read8(kbuf, at + p.value * 16 * (uint32_t)sizeof(T), lo[p.value]);
-            read8(kbuf, at + (D / 2 + p.value * 16) * (uint32_t)sizeof(T), up[p.value]);
+            eight(16 * p.value + 8 * hw, lo[p.value]);
+            eight(D / 2 + 16 * p.value + 8 * hw, up[p.value]);
         });
-        wave_turns<D>(rt.quarters, first - (cur_len - 1), own, lane);
+        if constexpr (STAGED) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // (read, before it is written again)
+        if constexpr (kt.value + 1 < KT) ask_keys(kt.value + 1);
+        wave_turns<D>(quarters, first - (cur_len - 1), own, lane);
         static_for<HP>([&](auto p) {
             static_for<8>([&](auto i) {
                 // (of finite values: a row that is not keeps to itself)
@@ -355,7 +397,7 @@ void k_weights(const WeightGeom, const _Float16* __restrict__ operands, const fl
         kfactor[kt.value] = pw.up;
         static_for<HP>([&](auto p) {
             float x[8], y[8], tc[8], ts[8];
-            seeds<D, 8>(rt.rows, own, l32, 16 * p.value + 8 * hw, tc, ts);
+            seeds<D, 8>(rows, own, l32, 16 * p.value + 8 * hw, tc, ts);
             static_for<8>([&](auto i) {
                 const float l = at8<i.value>(lo[p.value]) * pw.down, u = at8<i.value>(up[p.value]) * pw.down;
                 x[i.value] = fmaf(l, tc[i.value], -(u * ts[i.value]));
@@ -368,36 +410,56 @@ void k_weights(const WeightGeom, const _Float16* __restrict__ operands, const fl
             __builtin_amdgcn_sched_barrier(0);
         });
     });
+    lds_barrier();                                   // (all keys read, before queries are written there)
 
-    const int t0 = split * g.split_tiles, t1 = min(t0 + g.split_tiles, g.q_tiles), past = cur_len - g.q_len;      // past: row of the query at place 0
-    // which tiles of queries see a key of the wave: places go from place0 on, and from 0 again where a head's chunk ends
+    // ---- queries, tile by tile.  Places go from place0 on, and from 0 again where a head's chunk ends; `past` is the row of the query at place 0.
+    const int t0 = split * g.split_tiles, t1 = min(t0 + g.split_tiles, g.q_tiles), past = cur_len - g.q_len;
+    auto place_of = [&](int j) { return j - g.by_q.quotient(j) * g.q_len; };
+    auto last_row = [&](int t) {                     // of the queries of a tile
+        const int j0 = t * kWeightTile, n = min(kWeightTile, g.M - j0), place0 = place_of(j0);
+        return past + (place0 + n > g.q_len ? g.q_len - 1 : place0 + n - 1);
+    };
+    auto next = [&](int t) {                         // the next tile that sees a key of the workgroup
+        while (t < t1 && last_row(t) < first_row) ++t;
+        return t;
+    };
+    const char* const ops = (const char*)operands + (long long)unit * g.q_tiles * weight_operand_bytes(D);
+    auto ask = [&](int t, int slot) {
+        const char* const from = ops + (long long)t * weight_operand_bytes(D);
+        static_for<QN>([&](auto i) {
+            const uint32_t at = (uint32_t)((i.value * 4 + wave) * 1024);
+            lds_dma16((uint32_t)(uintptr_t)(lptr_t)pool + (uint32_t)(slot * QTILE) + at, from, at + (uint32_t)(lane * 16));
+        });
+        if (lane < kWeightTile * 8 / 16) lds_dma16((uint32_t)(uintptr_t)(lptr_t)&fsm[wave][slot][0], from, (uint32_t)(QTILE + lane * 16));
+    };
     f32x16 sum[KT];
     static_for<KT>([&](auto kt) { static_for<16>([&](auto r) { sum[kt.value][r.value] = 0.f; }); });
-    constexpr int AHEAD = 2;                         // k-steps that a tile's queries are asked for ahead of their use
-    const half8* const ops = (const half8*)(operands + (long long)unit * g.q_tiles * (2 * kWeightTile * D)) + lane;
-    half8 qh[AHEAD], ql[AHEAD];
-    auto ask = [&](int t, auto k) {
-        const half8* const op = ops + (long long)t * (2 * KS * 64);
-        qh[k.value % AHEAD] = op[k.value * 64];
-        ql[k.value % AHEAD] = op[(KS + k.value) * 64];
-    };
-    for (int t = t0; t < t1; ++t) {
-        const int j0 = t * kWeightTile, n = min(kWeightTile, g.M - j0), place0 = j0 - g.by_q.quotient(j0) * g.q_len;
-        const bool wraps = place0 + n > g.q_len;
-        if (row0 > past + (wraps ? g.q_len - 1 : place0 + n - 1)) continue;
-        static_for<AHEAD>([&](auto k) { ask(t, k); });
-        const float2 of_query = factors[((long long)unit * g.q_tiles + t) * kWeightTile + l32];
+    int ta = next(t0), tb = next(ta + 1);
+    if (ta < t1) ask(ta, 0);
+    if (tb < t1) ask(tb, 1);
+    for (int slot = 0; ta < t1;) {
+        const int tc = next(tb + 1), after = slot == 0 ? 2 : slot - 1;       // the slot of the tile before
+        if (tb < t1) landed(IC<QN + 1>{});
+        else landed(IC<0>{});
+        lds_barrier();
+        if (tc < t1) ask(tc, after);
+        const int t = ta, j0 = t * kWeightTile, place0 = place_of(j0);
+        const half8* const op = (const half8*)(pool + slot * QTILE) + lane;
+        const float2 of_query = fsm[wave][slot][l32];
+        ta = tb;
+        tb = tc;
+        slot = slot == 2 ? 0 : slot + 1;
+        if (row0 > last_row(t)) continue;            // no query of the tile sees a key of the wave
         f32x16 s[KT];
         static_for<KT>([&](auto kt) { static_for<16>([&](auto r) { s[kt.value][r.value] = 0.f; }); });
         static_for<KS>([&](auto k) {
-            const half8 h = qh[k.value % AHEAD], l = ql[k.value % AHEAD];
+            const half8 h = op[k.value * 64], l = op[(KS + k.value) * 64];
             static_for<KT>([&](auto kt) { s[kt.value] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kl[kt.value][k.value], h, s[kt.value], 0, 0, 0); });
             static_for<KT>([&](auto kt) { s[kt.value] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh[kt.value][k.value], l, s[kt.value], 0, 0, 0); });
             static_for<KT>([&](auto kt) { s[kt.value] = __builtin_amdgcn_mfma_f32_32x32x16_f16(kh[kt.value][k.value], h, s[kt.value], 0, 0, 0); });
-            if constexpr (k.value + AHEAD < KS) ask(t, IC<k.value + AHEAD>{});
         });
-        const bool masked = row0 + KEYS - 1 > past + (wraps ? 0 : place0);
-        const int at = j0 + l32, last = past + at - g.by_q.quotient(at) * g.q_len;       // row of the lane's query (one that there is not adds nothing)
+        const bool masked = row0 + KEYS - 1 > past + (place0 + min(kWeightTile, g.M - j0) > g.q_len ? 0 : place0);
+        const int last = past + place_of(j0 + l32);  // row of the lane's query (one that there is not adds nothing)
         static_for<KT>([&](auto kt) {
             const float f = kfactor[kt.value] * of_query.x;
             static_for<16>([&](auto r) {
@@ -728,26 +790,26 @@ hipError_t launch_weights_few(const SlabTable& tab, const WeightGeom& g, const v
     });
 }
 
-hipError_t launch_weights_queries(const WeightGeom& g, const void* q, const float* lse, const TurnTable& rt, void* operands, float2* factors, hipStream_t st)
+hipError_t launch_weights_queries(const WeightGeom& g, const void* q, const float* lse, const TurnTable& rt, void* operands, hipStream_t st)
 {
     WeightGeom h = g;
     h.by_split = divisor(g.q_tiles);
     return by_type(g, [&](auto t, auto d) {
         typedef decltype(t) T;
         hipLaunchKernelGGL((k_weights_queries<T, decltype(d)::value>), dim3((unsigned)(g.units * g.q_tiles)), dim3(256), 0, st, h, (const T*)q, lse, rt,
-                           (_Float16*)operands, factors);
+                           (char*)operands);
         return hipGetLastError();
     });
 }
 
-hipError_t launch_weights(const SlabTable& tab, const WeightGeom& g, const void* operands, const float2* factors, const TurnTable& rt, float* parts,
+hipError_t launch_weights(const SlabTable& tab, const WeightGeom& g, const void* operands, const TurnTable& rt, float* parts,
                           float* weights, hipStream_t st)
 {
     if (g.key_blocks != (g.cur_len + weight_keys(g.d) - 1) / weight_keys(g.d) || (long long)g.n_split * g.split_tiles < g.q_tiles) return hipErrorInvalidValue;
     hipError_t e = by_type(g, [&](auto t, auto d) {
         typedef decltype(t) T;
         hipLaunchKernelGGL((k_weights<T, decltype(d)::value>), dim3((unsigned)(g.units * g.n_split * g.key_blocks)), dim3(256), 0, st, g,
-                           (const _Float16*)operands, factors, rt, parts, weights, tab);
+                           (const _Float16*)operands, rt, parts, weights, tab);
         return hipGetLastError();
     });
     if (e != hipSuccess || g.n_split < 2) return e;

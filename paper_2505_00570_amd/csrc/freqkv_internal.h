@@ -418,12 +418,12 @@ struct WeightGeom {
     long long stride_batch, stride_head, stride_token;   // elements
     float qscale;                      // log2(e) / sqrt(d)
 };
-// operands: [unit][q_tiles][hi, lo][d / 16][64 lanes][8] fp16; factors: [unit][q_tiles][32] (factor of a score, -log2(e) lse)
-inline size_t weight_operand_bytes(int d) { return (size_t)kWeightTile * d * 4; }
+// operands: [unit][q_tiles] of: [hi, lo][d / 16][64 lanes][8] fp16, then [32] (factor of a score, -log2(e) lse)
+__host__ __device__ constexpr size_t weight_operand_bytes(int d) { return (size_t)kWeightTile * d * 4 + kWeightTile * 8; }
 hipError_t launch_weights_few(const SlabTable& tab, const WeightGeom& g, const void* q, const float* lse, const TurnTable& rt, float* weights, hipStream_t st);
-hipError_t launch_weights_queries(const WeightGeom& g, const void* q, const float* lse, const TurnTable& rt, void* operands, float2* factors, hipStream_t st);
+hipError_t launch_weights_queries(const WeightGeom& g, const void* q, const float* lse, const TurnTable& rt, void* operands, hipStream_t st);
 // parts: [n_split][units][cur_len] where n_split > 1
-hipError_t launch_weights(const SlabTable& tab, const WeightGeom& g, const void* operands, const float2* factors, const TurnTable& rt, float* parts,
+hipError_t launch_weights(const SlabTable& tab, const WeightGeom& g, const void* operands, const TurnTable& rt, float* parts,
                           float* weights, hipStream_t st);
 
 struct EvictGeom {
