@@ -1795,17 +1795,12 @@ freqkv_status_t q8_move(bool quantize, const void* k, const void* v, const freqk
     return FREQKV_OK;
 }
 
-// Whether operands written first are faster than k_attend_q8, which reads rows once for 16 queries.
-bool q8_prefill_pays(const PrefillShape& p)
-{
-    return p.a.G * p.q_len > 64;
-}
-
 struct Q8Shape {
     long long units_all, units;         // all; of a pass
     int M, parts, n_split, chunk;
     size_t ml_offset, workspace_bytes;
 
+    // chunks of the rows, ns of them or fewer
     void cut(long long ns, int cur_len, int d)
     {
         chunk = (int)round_up((cur_len + ns - 1) / ns, kQ8StepRows);
@@ -1831,21 +1826,36 @@ freqkv_status_t check_q8(const freqkv_layout_t* L, int q_dtype, int n_q, int n_k
     if (M >= 1 << 20 || s.units >= 1 << 20 || s.units_all * M >= 1LL << 31) return FREQKV_E_UNSUPPORTED;
     s.M = (int)M;
     s.parts = (s.M + kQ8Queries - 1) / kQ8Queries;
-    const long long most = (cur_len + kQ8StepRows - 1) / kQ8StepRows;
-    s.cut(std::min(most, std::max(1LL, 512 / (s.units * s.parts))), cur_len, d);
+    // Chunks for 256 workgroups or for 512, each of two steps at least; or none.  Two workgroups on a compute unit take 25/16 of the time of one for a step each (256 of 64 steps:
+    // 127 us, 512 of 32: 101); the merge takes two steps' time, and one more for every 4096 states.
+    // (16 x 56 queries on 912 rows: 4 chunks 12.9 us, 8 chunks 14.1; 32 x 36 on 2786: 2 chunks 26.7, 5 chunks 21.9; 32 x 96 on 1003: none 18.7, 2 chunks 21.5.)
+    const long long wgs = s.units * s.parts, steps = (cur_len + kQ8StepRows - 1) / kQ8StepRows;
+    long long cuts = 1, least = steps * std::max(wgs * 25 / 32, 256LL);
+    for (long long target : {256, 512}) {
+        const long long ns = std::min(target / wgs, (steps + 1) / 2);
+        if (ns < 2) continue;
+        const long long each = (steps + ns - 1) / ns, chunks = (steps + each - 1) / each;
+        const long long cost = each * std::max(wgs * chunks * 25 / 32, 256LL) + 2 * 256 + s.units * s.M * chunks / 16;
+        if (cost < least) { least = cost; cuts = ns; }
+    }
+    s.cut(cuts, cur_len, d);
     if (s.units * s.n_split >= 1 << 23) return FREQKV_E_UNSUPPORTED;
     *out = s;
     return FREQKV_OK;
 }
 
-// A chunk of many queries of bf16 over codes of 128 channels goes as over a bf16 cache, operands written first (the powers of two lie ahead of that way's workspace).
-bool q8_as_prefill(const freqkv_layout_t& L, int q_dtype, int n_q, int n_kv, int d, int cur_len, int q_len, bool ragged, PrefillShape* p)
+// A chunk of many queries of bf16 over codes of 128 channels goes as over a bf16 cache, operands written first (the powers of two lie ahead of that way's workspace), where
+// k_attend_q8, which reads the rows once for 16 queries, takes more: by its steps and what a workgroup costs besides, two and a half of them, in each round of 512 workgroups,
+// against a fixed part, and one by the length, of the other way.  (8 heads of 232 queries on 10631 rows: 56 us that way, 41 this one; 8 of 84 on 14063: 34 and 45;
+// 64 of 304 on 895: 51 and 31; 4 of 128 on 5989: 18 and 31; 128 of 96 on 116: 15.4 and 15.6.)
+bool q8_as_prefill(const freqkv_layout_t& L, int q_dtype, int n_q, int n_kv, int d, int cur_len, int q_len, bool ragged, const Q8Shape& s, PrefillShape* p)
 {
     if (q_dtype != FREQKV_BF16 || d != 128 || ragged || q_len < 2) return false;
     freqkv_layout_t rows = L;
     rows.dtype = FREQKV_BF16;
     if (check_prefill(&rows, n_q, n_kv, d, cur_len, q_len, p) != FREQKV_OK) return false;
-    return q8_prefill_pays(*p);
+    const long long rounds = (s.units * s.parts * s.n_split + 511) / 512, steps = (s.chunk + kQ8StepRows - 1) / kQ8StepRows;
+    return rounds * (2 * steps + 5) > 16 + cur_len / 512;
 }
 size_t powers_bytes(const PrefillShape& p) { return (size_t)round_up(p.units * (long long)sizeof(float2), 256); }
 
@@ -1957,7 +1967,7 @@ freqkv_status_t freqkv_attend_q8_plan(const freqkv_layout_t* layout8, int q_dtyp
     out->heads_together = std::min(s.M, kQ8Queries);
     out->workspace_bytes = s.workspace_bytes;
     PrefillShape p;
-    if (q8_as_prefill(*layout8, q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, false, &p))
+    if (q8_as_prefill(*layout8, q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, false, s, &p))
         out->workspace_bytes = std::max(out->workspace_bytes, p.workspace_bytes + powers_bytes(p));
     const double seen = (double)q_len * (cur_len - q_len) + 0.5 * (double)q_len * (q_len + 1);
     const double e = q_dtype == FREQKV_BF16 ? 2.0 : 4.0;
@@ -1984,7 +1994,7 @@ freqkv_status_t freqkv_attend_q8(const void* q, const void* k8, const void* v8, 
     if (!L.workspace || ((uintptr_t)L.workspace & 255)) return FREQKV_E_WORKSPACE;
     PrefillShape p;
     int split_tiles = 0;
-    if (q8_as_prefill(L, q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, cur_lens != nullptr, &p) && L.workspace_bytes >= powers_bytes(p) &&
+    if (q8_as_prefill(L, q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, cur_lens != nullptr, s, &p) && L.workspace_bytes >= powers_bytes(p) &&
         fit_prefill(&p, L.workspace_bytes - powers_bytes(p), &split_tiles) == FREQKV_OK)
         return attend_q8_prefill(p, split_tiles, bases, q, out, lse, L, *scales, shift, rope_base, (hipStream_t)stream);
     // (a workspace planned at another length: fewer chunks)
@@ -2039,7 +2049,7 @@ const char* freqkv_debug_attend_q8_kernel(const freqkv_layout_t* layout8, int q_
     Q8Shape s;
     PrefillShape p;
     if (check_q8(layout8, q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, &s) < 0) return nullptr;
-    return q8_as_prefill(*layout8, q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, ragged != 0, &p) ? "k_attend_prefill (operands of codes)" : "k_attend_q8";
+    return q8_as_prefill(*layout8, q_dtype, n_q_heads, n_kv_heads, head_dim, cur_len, q_len, ragged != 0, s, &p) ? "k_attend_prefill (operands of codes)" : "k_attend_q8";
 }
 
 freqkv_status_t freqkv_attend_weights_plan(const freqkv_layout_t* layout, int n_q_heads, int n_kv_heads, int head_dim, int cur_len, int q_len,

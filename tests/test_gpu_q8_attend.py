@@ -114,6 +114,32 @@ def test_chunks(T, n, d, G, dtype, fmt):
     _run(1, 2, 2, G, T, n, d, dtype, fmt, 32, seed=T + n)
 
 
+@pytest.mark.parametrize("L,B,H,G,T,n", [(1, 1, 64, 4, 200, 50), (2, 16, 4, 2, 71, 71), (1, 256, 1, 1, 300, 97), (3, 2, 40, 3, 40, 40), (98, 1, 4, 4, 65, 33)])
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("token_major", [False, True])
+def test_chunks_of_many_heads(L, B, H, G, T, n, fmt, token_major):
+    """Where operands are written first."""
+    L8 = binding.layout_for(torch.empty((L, B, H, T, 128), dtype=ref.CODES[fmt], device=DEV))
+    assert fk.attend_q8_kernel(L8, fk.BF16, H * G, H, 128, T, n) == "k_attend_prefill (operands of codes)"
+    _run(L, B, H, G, T, n, 128, torch.bfloat16, fmt, 32, seed=T + n, token_major=token_major)
+
+
+def test_nan_blocks_of_many_heads():
+    """The same as for few: a NaN scale makes NaN what sees its rows, and nothing else."""
+    T, n, block, H = 160, 60, 16, 100
+    q, k8, v8, scales = _case(1, 1, H, 2, T, n, 128, torch.bfloat16, "int8", block, 11)
+    assert fk.attend_q8_kernel(binding.layout_for(k8), fk.BF16, 2 * H, H, 128, T, n) == "k_attend_prefill (operands of codes)"
+    sees = 128 - (T - n)
+    good, _ = _attend(q, k8, v8, scales, block, T)
+    for which in range(2):
+        s = [x.clone() for x in scales]
+        s[which][0, 0, 1, 8] = math.nan
+        out, _ = _attend(q, k8, v8, s, block, T)
+        hit = torch.zeros(out.shape, dtype=torch.bool, device=DEV)
+        hit[:, :, 2:4, sees:] = True
+        assert torch.equal(out[~hit], good[~hit]) and bool(out[hit].isnan().all())
+
+
 @pytest.mark.parametrize("base", [0.0, 500000.0])
 @pytest.mark.parametrize("T", [777, 9000])
 def test_rotary_bases_and_long_caches(base, T):
@@ -169,8 +195,8 @@ def test_magnitudes(fmt, dtype, n):
 def test_magnitudes_of_operands(fmt):
     """The same where operands are written first: keys by 2^60, queries by 2^-60 and the other way round, values by 2^90 and 2^-90, blocks of a head 2^-10 .. 1 of each other."""
     T, block, n = 200, 32, 50
-    q, k8, v8, scales = _case(1, 1, 2, 4, T, n, 128, torch.bfloat16, fmt, block, 9)
-    assert fk.attend_q8_kernel(binding.layout_for(k8), fk.BF16, 8, 2, 128, T, n) == "k_attend_prefill (operands of codes)"
+    q, k8, v8, scales = _case(1, 1, 64, 4, T, n, 128, torch.bfloat16, fmt, block, 9)
+    assert fk.attend_q8_kernel(binding.layout_for(k8), fk.BF16, 256, 64, 128, T, n) == "k_attend_prefill (operands of codes)"
     lens = torch.full((1,), T, dtype=torch.int32, device=DEV)
     for e in (60, -60):
         ks = scales[0] * 2.0 ** e
@@ -213,7 +239,8 @@ def test_zero_queries_and_zero_blocks():
 def test_replayed_graph_of_a_chunk():
     """Operands written first: captured by a call that finds none of its tables, replayed on other codes and queries, with eager calls between."""
     T, block, n = 300, 32, 40
-    q, k8, v8, scales = _case(1, 2, 2, 4, T, n, 128, torch.bfloat16, "e4m3", block, 17)
+    q, k8, v8, scales = _case(1, 32, 2, 4, T, n, 128, torch.bfloat16, "e4m3", block, 17)
+    assert fk.attend_q8_kernel(binding.layout_for(k8), fk.BF16, 8, 2, 128, T, n) == "k_attend_prefill (operands of codes)"
     L8, S = ref.layouts8(k8, scales[0], scales[1], block)
     _, p = fk.attend_q8_plan(L8, fk.BF16, 8, 2, 128, T, n)
     ws = ref.with_workspace(L8, p.workspace_bytes)
