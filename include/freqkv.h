@@ -428,7 +428,7 @@ FREQKV_API freqkv_status_t freqkv_attend_weights_plan(const freqkv_layout_t* lay
  *   lse       [n_layers][batch][n_q_heads][q_len] fp32; a query whose lse is -inf adds nothing
  *   weights   [n_layers][batch][n_kv_heads][layout.token_capacity] fp32; rows at and beyond a sequence's length are left as they were
  *   cur_lens  optional DEVICE array [batch], as in freqkv_attend_q8; queries that sit ahead of row 0 add nothing
- *   layout.workspace  freqkv_attend_weights_plan(...).workspace_bytes, 256-byte aligned
+ *   layout.workspace  freqkv_attend_weights_plan(...).workspace_bytes, 256-byte aligned; with less the queries are cut into fewer parts, down to one
  * head_dim 64, 128 or 256.  Scores are good to 22 bits whatever the type; the order of the sums, and so their bits, depend on the sizes alone.
  */
 FREQKV_API freqkv_status_t freqkv_attend_weights(const void* q, const void* k, const float* lse, float* weights, const freqkv_layout_t* layout,

@@ -1906,6 +1906,14 @@ struct WeightShape {
     long long units;                    // of a pass
     int M, n_chunk, chunk, q_tiles, n_split, split_tiles, key_blocks;
     size_t off_parts, workspace_bytes;
+
+    // parts of the tiles of queries, ns of them or fewer
+    void cut(long long ns)
+    {
+        split_tiles = (int)((q_tiles + ns - 1) / ns);
+        n_split = (q_tiles + split_tiles - 1) / split_tiles;
+        workspace_bytes = off_parts + (n_split > 1 ? (size_t)n_split * units * a.cur_len * sizeof(float) : 0);
+    }
 };
 
 freqkv_status_t check_weights(const freqkv_layout_t* L, int n_q, int n_kv, int d, int cur_len, int q_len, WeightShape* out)
@@ -1930,12 +1938,9 @@ freqkv_status_t check_weights(const freqkv_layout_t* L, int n_q, int n_kv, int d
         w.q_tiles = (w.M + kWeightTile - 1) / kWeightTile;
         w.key_blocks = (cur_len + weight_keys(d) - 1) / weight_keys(d);
         const long long wgs = w.units * w.key_blocks;
-        const long long ns = std::min((long long)w.q_tiles, std::max(1LL, 1024 / wgs));
-        w.split_tiles = (int)((w.q_tiles + ns - 1) / ns);
-        w.n_split = (w.q_tiles + w.split_tiles - 1) / w.split_tiles;
-        if (wgs * w.n_split >= 1 << 23 || w.units * w.q_tiles >= 1 << 23) return FREQKV_E_UNSUPPORTED;
         w.off_parts = kTableBytes + (size_t)w.units * w.q_tiles * weight_operand_bytes(d);
-        w.workspace_bytes = w.off_parts + (w.n_split > 1 ? (size_t)w.n_split * w.units * cur_len * sizeof(float) : 0);
+        w.cut(std::min((long long)w.q_tiles, std::max(1LL, 1024 / wgs)));
+        if (wgs * w.n_split >= 1 << 23 || w.units * w.q_tiles >= 1 << 23) return FREQKV_E_UNSUPPORTED;
     }
     *out = w;
     return FREQKV_OK;
@@ -2084,7 +2089,10 @@ freqkv_status_t freqkv_attend_weights(const void* q, const void* k, const float*
     const freqkv_layout_t& L = *layout;
     std::vector<char*> bases;
     if (!layer_bases(k, k, L, w.a.elem, &bases)) return FREQKV_E_INVALID;
-    if (!L.workspace || ((uintptr_t)L.workspace & 255) || L.workspace_bytes < w.workspace_bytes) return FREQKV_E_WORKSPACE;
+    if (!L.workspace || ((uintptr_t)L.workspace & 255)) return FREQKV_E_WORKSPACE;
+    // (a workspace planned at another length: fewer parts)
+    while (w.n_split > 1 && w.workspace_bytes > L.workspace_bytes) w.cut(w.n_split - 1);
+    if (L.workspace_bytes < w.workspace_bytes) return FREQKV_E_WORKSPACE;
     char* const ws = (char*)L.workspace;
     hipStream_t st = (hipStream_t)stream;
     RopeEntry* rope = nullptr;

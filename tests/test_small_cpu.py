@@ -2,6 +2,7 @@
 import ctypes as C
 
 import pytest
+import torch
 
 import paper_2505_00570_amd as fk
 from paper_2505_00570_amd import binding
@@ -126,3 +127,21 @@ def test_plans():
                     assert p.bytes_algorithmic == 12 * (2 * cur * d + 2 * 3 * n * d * (2 if dt == fk.BF16 else 4))
                 _, p = fk.attend_weights_plan(L, 6, 2, d, cur, n)
                 assert p.flops == 2.0 * d * seen * 6 * 6 and p.workspace_bytes >= 35840
+
+
+def test_caches_ask_for_what_their_calls_need():
+    """Workspaces and buffers of the two caches that are kept small, and what their makers refuse."""
+    from paper_2505_00570_amd.cache import CompressedKVCache, QuantizedKVCache
+    c = CompressedKVCache(2, 1, 2, 64, 100, n_q_heads=8, by_weight=True, n_recent=10, device="cpu")
+    assert c.weights.shape == (2, 1, 2, 100) and not bool(c.weights.any()) and c.kept.shape == (2, 1, 2, 38)
+    assert c.compress() == binding.NOOP and c.cur_len == 0
+    for n_recent in (-1, 48):
+        with pytest.raises(ValueError):
+            CompressedKVCache(2, 1, 2, 64, 100, by_weight=True, n_recent=n_recent, device="cpu")
+    for code in (torch.int8, torch.float8_e4m3fn):
+        c = QuantizedKVCache(5, 1, 2, 64, 100, n_q_heads=8, device="cpu", code_dtype=code, stage_layers=2)
+        assert c.compress() == binding.NOOP and c.k_scale.shape == (5, 1, 2, 2) and c.stage_k.shape[0] == 2
+        for n, q_len in ((1, 1), (50, 1), (100, 1), (100, 37), (100, 100)):
+            # (a smaller one than planned is used all the same: down to that of one chunk)
+            assert c.layout.workspace_bytes >= 35840
+            assert fk.attend_q8_plan(c.layout, fk.BF16, 8, 2, 64, n, q_len)[1].workspace_bytes <= c.layout.workspace_bytes
