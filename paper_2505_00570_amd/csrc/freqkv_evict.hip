@@ -531,18 +531,6 @@ __device__ __forceinline__ int sum16(int x)
     return __builtin_amdgcn_readfirstlane(x);
 }
 
-// Sum over the wave, in its last lane.
-__device__ __forceinline__ int sum_wave(int x)
-{
-    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);       // lanes 1, 2, 4 and 8 below, in rows of 16
-    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
-    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // the last lane of a row to the next
-    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // ... of the second row to the third and fourth
-    return x;
-}
-
 // Rows of a sequence and of what competes in it.
 struct Span { int n, lo, hi; bool due; };
 __device__ __forceinline__ Span span_of(const EvictGeom& g, int b)
@@ -559,7 +547,7 @@ __device__ __forceinline__ Span span_of(const EvictGeom& g, int b)
 
 // A workgroup to a unit, a thread with R rows of its own, 1024 apart, in registers (R 0: more rows than that, read again each time).  The keep-th largest order is
 // found bit by bit, from counts of the rows at or above a candidate, until just the rows that stay are (with counters in LDS, rows of much the same weight queue
-// for the same one: 8192 rows 22 us, so 13.8, or 17.5 where equal weights take all 32 bits; two bits at a time 28); of the rows that have it the first ones stay.  Then every row that stays has its place from the counts of those before
+// for the same one: 8192 rows 22 us, so 14, or 17 where equal weights take all 32 bits; two bits at a time 28); of the rows that have it the first ones stay.  Then every row that stays has its place from the counts of those before
 // it, by 64s, which a scan gives.  weights_out may be weights: all rows are read ahead of a barrier.
 template <int R>
 __global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictGeom, const float* weights, float* weights_out, int* __restrict__ kept, int* __restrict__ new_lens)
@@ -567,9 +555,10 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictGeom
     const EvictGeom g = first_argument<decltype(k_evict_select<R>)>();
     constexpr int W = kSelectWaves, N = R ? R : 1;
     static_assert(W == 16, "a count to each lane of 16");
-    __shared__ __attribute__((aligned(16))) int counts[2][2][W];
+    __shared__ int counts[2][2][W];                  // R 0
     __shared__ int larger[N * W], equal[N * W];      // of each 64 rows, then of all rows before them
     __shared__ int sums[2][W];
+    __shared__ int totals[32];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int unit = blockIdx.x, layer = g.by_layer.quotient(unit), rem = unit - layer * g.units_per_layer;
     const int b = g.by_kv.quotient(rem), kvh = rem - b * g.n_kv;
@@ -589,6 +578,8 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictGeom
         return;
     }
     const int rows = s.hi - s.lo, tiles = (rows + kSelectThreads - 1) / kSelectThreads;
+    if (tid < 32) totals[tid] = 0;
+    __syncthreads();
     float x[N];
     uint32_t u[N];
     static_for<R>([&](auto i) { const int r = i.value * kSelectThreads + tid; x[i.value] = r < rows ? w[s.lo + r] : 0.f; });
@@ -607,14 +598,13 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictGeom
         }
     };
     uint32_t found = 0;
-    for (int bit = 31, flip = 0; bit >= 0; --bit, flip ^= 1) {
+    for (int bit = 31; bit >= 0; --bit) {
         const uint32_t candidate = found | 1u << bit;
         int n = 0;
-        each([&](int, bool, uint32_t v, float) { n += v >= candidate; });
-        n = sum_wave(n);
-        if (lane == 63) counts[flip][0][wave] = n;
-        __syncthreads();
-        n = sum16(counts[flip][0][lane & 15]);
+        each([&](int, bool, uint32_t v, float) { n += __popcll(__builtin_amdgcn_ballot_w64(v >= candidate)); });
+        if (lane == 0) atomicAdd(&totals[bit], n);
+        lds_barrier();
+        n = __builtin_amdgcn_readfirstlane(totals[bit]);
         if (n >= g.keep) found = candidate;
         if (n == g.keep) {                           // just the rows that stay: all above the next lower order
             --found;
