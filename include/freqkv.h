@@ -384,7 +384,8 @@ typedef struct freqkv_scales {
  * may come one by one, and each stays within one step of the block's scale (int8; e4m3 codes but lose bits below its least exponent) of what it was.
  * Quotients are rounded to the nearest code, ties to the even one, exactly.  Where a value of the new rows of a block is infinite or NaN the block's scale becomes NaN,
  * and its values with it.  Rows behind code_row + n_rows of the last block are not looked at or written.
- * head_dim a multiple of 16, up to 256 (FREQKV_E_UNSUPPORTED otherwise); both layouts have the same n_layers and batch.  No workspace.  n_rows 0: FREQKV_NOOP.
+ * head_dim a multiple of 16, up to 256 (FREQKV_E_UNSUPPORTED otherwise); both layouts have the same n_layers and batch.  K, V and layers that are written
+ * have addresses of their own (so here scales of K and V).  No workspace.  n_rows 0: FREQKV_NOOP.
  */
 FREQKV_API freqkv_status_t freqkv_quantize(const void* k, const void* v, const freqkv_layout_t* layout, int row, void* k8, void* v8,
                                 const freqkv_layout_t* layout8, const freqkv_scales_t* scales, int code_row, const int32_t* code_rows /* device */,
@@ -445,7 +446,7 @@ FREQKV_API freqkv_status_t freqkv_attend_weights(const void* q, const void* k, c
  *   kept         [n_layers][batch][n_heads][keep] int32: rows that stayed, ascending; where nothing moved the rows that competed, and -1 behind them
  *   cur_lens     optional DEVICE array [batch] of int32, clamped to [0, cur_len], cur_len then being their upper bound
  *   new_lens     optional DEVICE array [batch] of int32: rows of each sequence after the call; not cur_lens itself
- * head_dim a multiple of 8; keep >= 1.  After the call rows at and beyond a sequence's new length hold unspecified values.  No workspace.
+ * head_dim a multiple of 8; keep >= 1; K, V and layers have addresses of their own.  After the call rows at and beyond a sequence's new length hold unspecified values.  No workspace.
  */
 FREQKV_API freqkv_status_t freqkv_evict(void* k, void* v, const float* weights, float* weights_out, int32_t* kept, const freqkv_layout_t* layout, int n_heads,
                              int head_dim, int cur_len, int n_sink, int n_recent, int keep, const int32_t* cur_lens /* device */,

@@ -1723,6 +1723,13 @@ bool layer_bases(const void* k, const void* v, const freqkv_layout_t& L, int ele
     return true;
 }
 
+// Whether no two of K and V of all layers start at the same address: what is written in place must not be written twice at once.
+bool all_apart(std::vector<char*> bases)
+{
+    std::sort(bases.begin(), bases.end());
+    return std::adjacent_find(bases.begin(), bases.end()) == bases.end();
+}
+
 constexpr int kLayersPerPass = kMaxSlabs / 2;
 
 void slabs_of(const std::vector<char*>& bases, int l0, int layers, SlabTable* tab)
@@ -1749,6 +1756,7 @@ freqkv_status_t q8_move(bool quantize, const void* k, const void* v, const freqk
     std::vector<char*> bases, bases8;
     if (!layer_bases(k, v, *layout, elem, &bases) || !layer_bases(k8, v8, *layout8, 1, &bases8)) return FREQKV_E_INVALID;
     if (n_rows == 0) return FREQKV_NOOP;
+    if (!all_apart(quantize ? bases8 : bases) || (quantize && (scales->k == scales->v || (layout8->n_layers > 1 && scales->stride_layer == 0)))) return FREQKV_E_INVALID;
 
     Q8MoveGeom g;
     memset(&g, 0, sizeof(g));
@@ -2141,7 +2149,7 @@ freqkv_status_t freqkv_evict(void* k, void* v, const float* weights, float* weig
     const freqkv_layout_t& L = *layout;
     const int elem = L.dtype == FREQKV_BF16 ? 2 : 4;
     std::vector<char*> bases;
-    if (!layer_bases(k, v, L, elem, &bases)) return FREQKV_E_INVALID;
+    if (!layer_bases(k, v, L, elem, &bases) || !all_apart(bases)) return FREQKV_E_INVALID;
     EvictGeom g;
     memset(&g, 0, sizeof(g));
     g.row_bytes = head_dim * elem;

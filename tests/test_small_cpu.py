@@ -145,3 +145,16 @@ def test_caches_ask_for_what_their_calls_need():
             # (a smaller one than planned is used all the same: down to that of one chunk)
             assert c.layout.workspace_bytes >= 35840
             assert fk.attend_q8_plan(c.layout, fk.BF16, 8, 2, 64, n, q_len)[1].workspace_bytes <= c.layout.workspace_bytes
+
+
+def test_what_is_written_twice_is_refused():
+    """K and V, or two layers, at one address: rows moved or rounded in place by two workgroups at once."""
+    inv, far = binding.E_INVALID, FAKE + (1 << 20)
+    apart = _set(_scales(), v=far)
+    assert _quantize(v8=far) == inv and _quantize(S=apart) == inv                   # scales; codes
+    assert _quantize(S=_set(_set(_scales(), v=far), stride_layer=0), v8=far) == inv
+    assert _quantize(L8=_set(_layout(fk.INT8), stride_layer=0), S=apart, v8=far) == inv
+    assert _dequantize() == inv and _dequantize(v=far, L=_set(_layout(fk.F32), stride_layer=0)) == inv
+    assert _evict() == inv and _evict(v=far, L=_set(_layout(fk.BF16), stride_layer=0)) == inv
+    table = (C.c_void_p * 2)(FAKE, far)
+    assert _evict(k=table, v=table, L=_set(_layout(fk.BF16), pointer_table=1)) == inv
