@@ -1853,17 +1853,20 @@ freqkv_status_t check_q8(const freqkv_layout_t* L, int q_dtype, int n_q, int n_k
 }
 
 // A chunk of many queries of bf16 over codes of 128 channels goes as over a bf16 cache, operands written first (the powers of two lie ahead of that way's workspace), where
-// k_attend_q8, which reads the rows once for 16 queries, takes more: by its steps and what a workgroup costs besides, two and a half of them, in each round of 512 workgroups,
-// against a fixed part, and one by the length, of the other way.  (8 heads of 232 queries on 10631 rows: 56 us that way, 41 this one; 8 of 84 on 14063: 34 and 45;
-// 64 of 304 on 895: 51 and 31; 4 of 128 on 5989: 18 and 31; 128 of 96 on 116: 15.4 and 15.6.)
+// k_attend_q8, which reads the rows once for 16 queries, takes more.  Microseconds, measured over 140 shapes: k_attend_q8 5 for each round of 512 workgroups and 2.1 for each
+// of their steps (1.3 where no two share a compute unit); the other way 15, the length's part, and what it writes and multiplies.
+// (8 heads of 232 queries on 10631 rows: 56 us that way, 41 this one; 64 of 304 on 895: 51 and 31; 256 of 104 on 174: 36 and 24; 8 of 84 on 14063: 34 and 45; 4 of 128 on 5989: 18 and 31;
+// 64 of 30 on 11291: 67 and 223; 128 of 128 on 4733: 178 and 188.)
 bool q8_as_prefill(const freqkv_layout_t& L, int q_dtype, int n_q, int n_kv, int d, int cur_len, int q_len, bool ragged, const Q8Shape& s, PrefillShape* p)
 {
     if (q_dtype != FREQKV_BF16 || d != 128 || ragged || q_len < 2) return false;
     freqkv_layout_t rows = L;
     rows.dtype = FREQKV_BF16;
     if (check_prefill(&rows, n_q, n_kv, d, cur_len, q_len, p) != FREQKV_OK) return false;
-    const long long rounds = (s.units * s.parts * s.n_split + 511) / 512, steps = (s.chunk + kQ8StepRows - 1) / kQ8StepRows;
-    return rounds * (2 * steps + 5) > 16 + cur_len / 512;
+    const long long wgs = s.units * s.parts * s.n_split, rounds = (wgs + 511) / 512, steps = s.chunk / kQ8StepRows;
+    const double all_rows = (double)s.units * cur_len;
+    const double here = 5.0 + (double)rounds * (5.0 + (wgs <= 256 ? 1.3 : 2.1) * (double)steps);
+    return here > 15.0 + cur_len / 625.0 + all_rows / 5000.0 + all_rows * p->a.G * p->q_pad / 2e6;
 }
 size_t powers_bytes(const PrefillShape& p) { return (size_t)round_up(p.units * (long long)sizeof(float2), 256); }
 
@@ -2152,8 +2155,7 @@ freqkv_status_t freqkv_evict(void* k, void* v, const float* weights, float* weig
     if (!layer_bases(k, v, L, elem, &bases) || !all_apart(bases)) return FREQKV_E_INVALID;
     EvictGeom g;
     memset(&g, 0, sizeof(g));
-    g.row_bytes = head_dim * elem;
-    g.row_pieces = g.row_bytes / 16;
+    g.row_pieces = head_dim * elem / 16;
     const int upl = L.batch * n_heads;
     const long long units = (long long)std::min(L.n_layers, kLayersPerPass) * L.batch * n_heads;
     if (units >= 1 << 20 || (long long)cur_len * g.row_pieces >= 1LL << 30) return FREQKV_E_UNSUPPORTED;

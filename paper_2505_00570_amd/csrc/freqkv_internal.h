@@ -427,7 +427,7 @@ hipError_t launch_weights(const SlabTable& tab, const WeightGeom& g, const void*
                           float* weights, hipStream_t st);
 
 struct EvictGeom {
-    int row_bytes, row_pieces;         // of a head's row; in pieces of 16 bytes
+    int row_pieces;                    // of a head's row, of 16 bytes
     int slices, slice_pieces;          // a workgroup moves slice_pieces pieces of every row
     int n_kv, units, units_per_layer;
     int cur_len, n_sink, n_recent, keep;
