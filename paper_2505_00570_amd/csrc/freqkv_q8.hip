@@ -93,11 +93,11 @@ constexpr int kMoveThreads = 256;
 // once, bound by memory: K and V of 8 heads of 8192 rows, bf16 to int8, 16.9 us, of bytes that a copy moves in 10.  A block that holds rows already keeps its scale, or has it doubled until the new rows fit, and its older codes are rounded again (so that
 // a row's error is below one step of the block's scale, whatever the number of calls that filled it; a new scale for every row that is
 // a little larger would round all rows again each time).
-template <int FMT, int E, int PIECES>
-__global__ __launch_bounds__(kMoveThreads) void k_quantize(const Q8MoveGeom, const SlabTable rows, const SlabTable codes)
+template <int FMT, int E, int PIECES, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_quantize(const Q8MoveGeom, const SlabTable rows, const SlabTable codes)
 {
-    const Q8MoveGeom g = first_argument<decltype(k_quantize<FMT, E, PIECES>)>();
-    __shared__ uint32_t most[kMoveThreads / 64];
+    const Q8MoveGeom g = first_argument<decltype(k_quantize<FMT, E, PIECES, THREADS>)>();
+    __shared__ uint32_t most[THREADS / 64];
     const int tid = threadIdx.x, slab = blockIdx.y;
     const int ht = g.by_blk.quotient(blockIdx.x), i = blockIdx.x - ht * g.n_blk;
     const int b = g.by_heads.quotient(ht), h = ht - b * g.n_heads;
@@ -119,7 +119,7 @@ __global__ __launch_bounds__(kMoveThreads) void k_quantize(const Q8MoveGeom, con
     u32x4 x[PIECES][E / 2];
     uint32_t bits = 0;
     static_for<PIECES>([&](auto p) {
-        const int piece = tid + p.value * kMoveThreads;
+        const int piece = tid + p.value * THREADS;
         static_for<E / 2>([&](auto j) { x[p.value][j.value] = u32x4{0u, 0u, 0u, 0u}; });
         if (piece < pieces) {
             const int row = g.by_pieces.quotient(piece);
@@ -130,9 +130,11 @@ __global__ __launch_bounds__(kMoveThreads) void k_quantize(const Q8MoveGeom, con
         static_for<8>([&](auto j) { bits = max(bits, __float_as_uint(value8(x[p.value], j.value)) & 0x7fffffffu); });
     });
     for (int o = 32; o; o >>= 1) bits = max(bits, (uint32_t)__shfl_xor((int)bits, o));
-    if ((tid & 63) == 0) most[tid >> 6] = bits;
-    __syncthreads();
-    static_for<kMoveThreads / 64>([&](auto w) { bits = max(bits, most[w.value]); });
+    if constexpr (THREADS > 64) {
+        if ((tid & 63) == 0) most[tid >> 6] = bits;
+        __syncthreads();
+        static_for<THREADS / 64>([&](auto w) { bits = max(bits, most[w.value]); });
+    }
     const float amax = __uint_as_float(bits);
 
     // the block's scale after the call, and by how many doublings an older one grows
@@ -153,7 +155,7 @@ __global__ __launch_bounds__(kMoveThreads) void k_quantize(const Q8MoveGeom, con
     const bool none = !(scale > 0.f);
     const float inverse = none ? 0.f : 1.f / scale;
     static_for<PIECES>([&](auto p) {
-        const int piece = tid + p.value * kMoveThreads;
+        const int piece = tid + p.value * THREADS;
         if (piece >= pieces) return;
         const int row = g.by_pieces.quotient(piece);
         u32x2 w;
@@ -166,7 +168,7 @@ __global__ __launch_bounds__(kMoveThreads) void k_quantize(const Q8MoveGeom, con
     });
     if (doubled > 0 && !none) {
         const float shrink = doubled > 100 ? 0.f : ldexpf(1.f, -doubled);
-        for (int piece = tid; piece < (lo - first) * per_row; piece += kMoveThreads) {
+        for (int piece = tid; piece < (lo - first) * per_row; piece += THREADS) {
             const int row = g.by_pieces.quotient(piece);
             u32x2* const at = (u32x2*)(to + (long long)row * g.code_token + (piece - row * per_row) * 8);
             u32x2 w = *at;
@@ -772,12 +774,15 @@ void k_attend_q8(const Q8AttGeom, const void* __restrict__ q, const TurnTable ta
 template <int FMT, int E>
 static hipError_t launch_quantize_t(const SlabTable& rows, const SlabTable& codes, const Q8MoveGeom& g, int slabs, hipStream_t st)
 {
-    const dim3 grid((unsigned)(g.n_blk * g.hts), (unsigned)slabs), block(kMoveThreads);
-    const int tokens = 1 << g.block_shift, need = ((tokens < g.n_rows ? tokens : g.n_rows) * (g.d / 8) + kMoveThreads - 1) / kMoveThreads;
-    auto launch = [&](auto pieces) {
-        hipLaunchKernelGGL((k_quantize<FMT, E, decltype(pieces)::value>), grid, block, 0, st, g, rows, codes);
+    const dim3 grid((unsigned)(g.n_blk * g.hts), (unsigned)slabs);
+    const int tokens = 1 << g.block_shift, pieces = (tokens < g.n_rows ? tokens : g.n_rows) * (g.d / 8), need = (pieces + kMoveThreads - 1) / kMoveThreads;
+    auto launch_of = [&](auto pieces, auto threads) {
+        hipLaunchKernelGGL((k_quantize<FMT, E, decltype(pieces)::value, decltype(threads)::value>), grid, dim3(threads.value), 0, st, g, rows, codes);
         return hipGetLastError();
     };
+    auto launch = [&](auto n) { return launch_of(n, IC<kMoveThreads>{}); };
+    // a wave to a block where it has a piece for each lane, at most: no barrier, and a fourth of the waves (a token of 32 layers x 8 sequences x 8 heads: 6.7 us, of four waves 9.1)
+    if (pieces <= 64) return launch_of(IC<1>{}, IC<64>{});
     if (need <= 1) return launch(IC<1>{});
     if (need <= 2) return launch(IC<2>{});
     if (need <= 4) return launch(IC<4>{});
