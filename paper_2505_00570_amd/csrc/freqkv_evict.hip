@@ -513,6 +513,7 @@ __global__ __launch_bounds__(256) void k_weights_join(const WeightGeom g, const 
 namespace {
 
 constexpr int kSelectThreads = 1024, kSelectWaves = kSelectThreads / 64;
+constexpr int kSelectBins = 2048, kSelectCopies = 4; // of a digit of 11 bits, two to a thread; of each count, one for each fourth lane
 
 // Larger weights have larger orders; +0 and -0 the same one, NaN the least.
 __device__ __forceinline__ uint32_t order_of(float w)
@@ -532,6 +533,18 @@ __device__ __forceinline__ int sum16(int x)
     return __builtin_amdgcn_readfirstlane(x);
 }
 
+// Sums over the lanes up to each.
+__device__ __forceinline__ int scan_wave(int x)
+{
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, true);       // lanes 1, 2, 4 and 8 below, in rows of 16
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, true);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);      // the last lane of a row to the next
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);      // ... of the second row to the third and fourth
+    return x;
+}
+
 // Rows of a sequence and of what competes in it.
 struct Span { int n, lo, hi; bool due; };
 __device__ __forceinline__ Span span_of(const EvictGeom& g, int b)
@@ -546,20 +559,23 @@ __device__ __forceinline__ Span span_of(const EvictGeom& g, int b)
 
 }  // namespace
 
-// A workgroup to a unit, a thread with R rows of its own, 1024 apart, in registers (R 0: more rows than that, read again each time).  The keep-th largest order is
-// found bit by bit, from counts of the rows at or above a candidate, until just the rows that stay are (with counters in LDS, rows of much the same weight queue
-// for the same one: 8192 rows 22 us, so 14, or 17 where equal weights take all 32 bits; two bits at a time 28); of the rows that have it the first ones stay.  Then every row that stays has its place from the counts of those before
-// it, by 64s, which a scan gives.  weights_out may be weights: all rows are read ahead of a barrier.
+// A workgroup to a unit, a thread with R rows of its own, 1024 apart, in registers (R 0: more rows than that, read again each time).  The keep-th largest order is found
+// by its digits, of 11, 11 and 10 bits, from counts in LDS of the rows that have each and the digits before it as found, until just the rows that stay are; of the rows that have
+// it the first ones stay.  Four counts of each digit, for lanes four apart and in different banks: rows of the same weight queue for one of them (8 heads of 8192 rows, of any weights
+// 9.2 us, all equal 13; with one count 9.1 and 28; digits of one bit, counted by ballots, 14 and 17; of eight, with their few exponents, 22).  Bound by the three rounds of counts,
+// barriers and sums.  Then every row that stays has its place from the counts of those before it, by 64s, which a scan gives.  weights_out may be weights: all rows are read ahead of
+// a barrier.
 template <int R>
 __global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictGeom, const float* weights, float* weights_out, int* __restrict__ kept, int* __restrict__ new_lens)
 {
     const EvictGeom g = first_argument<decltype(k_evict_select<R>)>();
     constexpr int W = kSelectWaves, N = R ? R : 1;
-    static_assert(W == 16, "a count to each lane of 16");
+    static_assert(W == 16 && kSelectBins == 2 * kSelectThreads, "a count to each lane of 16; two digits to a thread");
     __shared__ int counts[2][2][W];                  // R 0
     __shared__ int larger[N * W], equal[N * W];      // of each 64 rows, then of all rows before them
     __shared__ int sums[2][W];
-    __shared__ int totals[32];
+    __shared__ __attribute__((aligned(16))) int bins[kSelectCopies][kSelectBins + 8];      // (copies of a digit's count in different banks)
+    __shared__ int digit[3];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int unit = blockIdx.x, layer = g.by_layer.quotient(unit), rem = unit - layer * g.units_per_layer;
     const int b = g.by_kv.quotient(rem), kvh = rem - b * g.n_kv;
@@ -579,7 +595,7 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictGeom
         return;
     }
     const int rows = s.hi - s.lo, tiles = (rows + kSelectThreads - 1) / kSelectThreads;
-    if (tid < 32) totals[tid] = 0;
+    static_for<kSelectCopies>([&](auto c) { *(u32x2*)&bins[c.value][2 * tid] = u32x2{0u, 0u}; });
     __syncthreads();
     float x[N];
     uint32_t u[N];
@@ -599,19 +615,41 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictGeom
         }
     };
     uint32_t found = 0;
-    for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t candidate = found | 1u << bit;
-        int n = 0;
-        each([&](int, bool, uint32_t v, float) { n += __popcll(__builtin_amdgcn_ballot_w64(v >= candidate)); });
-        if (lane == 0) atomicAdd(&totals[bit], n);
+    int need = g.keep;                               // of the rows whose upper bits are found's
+    static_for<3>([&](auto pass) {
+        constexpr int SHIFT = pass.value == 0 ? 21 : pass.value == 1 ? 10 : 0, BITS = pass.value == 2 ? 10 : 11;
+        if (need == 0) return;
+        each([&](int, bool there, uint32_t v, float) {
+            if (there && (pass.value == 0 || ((v ^ found) >> SHIFT) >> BITS == 0)) atomicAdd(&bins[lane & (kSelectCopies - 1)][v >> SHIFT & ((1 << BITS) - 1)], 1);
+        });
         lds_barrier();
-        n = __builtin_amdgcn_readfirstlane(totals[bit]);
-        if (n >= g.keep) found = candidate;
-        if (n == g.keep) {                           // just the rows that stay: all above the next lower order
-            --found;
-            break;
+        // a thread has two digits, the largest ones first; the rows of those before them
+        const int d0 = kSelectBins - 1 - 2 * tid;
+        int c0 = 0, c1 = 0;
+        static_for<kSelectCopies>([&](auto c) {
+            u32x2* const both = (u32x2*)&bins[c.value][d0 - 1];
+            c0 += (int)(*both)[1];
+            c1 += (int)(*both)[0];
+            *both = u32x2{0u, 0u};
+        });
+        const int upto = scan_wave(c0 + c1);
+        if (lane == 63) counts[0][0][wave] = upto;
+        lds_barrier();
+        const int before = upto - c0 - c1 + sum16((lane & 15) < wave ? counts[0][0][lane & 15] : 0);
+        if (before < need && need <= before + c0 + c1) {
+            const bool first = need <= before + c0;
+            digit[0] = first ? d0 : d0 - 1;
+            digit[1] = first ? before : before + c0;     // rows above it
+            digit[2] = first ? c0 : c1;
         }
-    }
+        lds_barrier();
+        found |= (uint32_t)__builtin_amdgcn_readfirstlane(digit[0]) << SHIFT;
+        need -= __builtin_amdgcn_readfirstlane(digit[1]);
+        if (need == __builtin_amdgcn_readfirstlane(digit[2]) && found > 0) {       // just the rows that stay: all above the next lower order
+            --found;
+            need = 0;
+        }
+    });
     // ---- rows above and at the order found, by 64s; `place` of the first row that stays of each
     auto prefix = [&](int i, int& above, int& at) {  // counts of a tile's waves, and those before
         above = larger[(R ? i : 0) * W + wave];
